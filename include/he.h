@@ -11,10 +11,10 @@
  *    drops limb limbs-1.  Inputs outside [0, q_i) are not detected and give undefined residues.
  *  - "dev" pointers are device (HBM) addresses on the context's GPU, 8-byte aligned; "host"
  *    pointers are ordinary host memory.  The caller owns every buffer; the library allocates device
- *    memory only in he_ctx_create and he_plan_create.
+ *    memory only in he_ctx_create, he_plan_create and he_i8_layer_create.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All device work is
  *    enqueued on it and no call synchronises with the device, except he_ctx_create,
- *    he_plan_create and the two destroy calls.
+ *    he_plan_create, he_i8_layer_create and the destroy calls.
  *  - Every call returns HE_OK (0) or a negative he_status; nothing aborts or throws.  Arguments,
  *    sizes and launch shapes are all checked before the first launch: on any status other than
  *    HE_ERR_DEVICE no device work has been enqueued by that call.  HE_ERR_DEVICE reports a failed HIP
@@ -226,9 +226,39 @@ int he_ct_square_relin(he_ctx* ctx, uint32_t limbs, const uint64_t* ct_in, uint3
                        uint64_t* ct_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Layers of 8-bit integer weights on ciphertexts, the matrix product of a quantised model: for every output o, modulo each
+ * limb's q and on both components,
+ *   out[o] = token_scale * (s_o * sum over t in [off[o], off[o+1]) of weights[term_pt[t]] * ct_in[term_ct[t]]) + bias[o],
+ * the bias on component 0 only.  The weights are whole numbers in [-128, 127] and carry no encoding scale; the scales that
+ * quantisation leaves are
+ *   per channel: s_o = the scalar encoding (Alg. 2) of channel_scale[o] * scale, fixed with the layer; without channel_scale
+ *                s_o = 1, and the message keeps its scale;
+ *   per token:   token_scale dev [limbs][N], a plaintext polynomial in NTT form (he_encode_vector): in a batch-axis packed
+ *                tensor a token is a slot, so one polynomial holds a scale for each of them.  NULL: none.
+ * The message's scale is multiplied by `scale` and by the scale at which token_scale was encoded; one HE_RESCALE serves both.
+ * The residues are the same as he_ct_pt_mac's with plaintexts s_o * weight (mod q); eight times less arithmetic is done for them.
+ *
+ * he_i8_layer_create: arrays as in he_plan_create; weights host [n_pt], channel_scale host [n_out] or NULL (non-finite products:
+ * HE_ERR_ARG); all are copied, laid out for the kernels and kept on the context's GPU.  A layer serves every level.  At most
+ * 131071 terms per output (HE_ERR_RANGE; longer sums go over several layers with HE_ACCUMULATE).  Takes device memory of about
+ * 32 bytes per term and group of up to 32 outputs with the same inputs (groups with the same weights share it), and 48 bytes per
+ * output and limb.  he_i8_layer_destroy is valid also after the context was destroyed.
+ *
+ * he_ct_i8_mac: ct_in, ct_out, bias, flags, workspace and the rule against overlaps as in he_ct_pt_mac (he_i8_workspace_bytes: the
+ * accumulators with HE_RESCALE, else 0, and then workspace may be NULL).
+ */
+typedef struct he_i8_layer he_i8_layer;
+int he_i8_layer_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt, const uint32_t* off, const uint32_t* term_ct,
+                       const uint32_t* term_pt, const int8_t* weights, const double* channel_scale, double scale, he_i8_layer** out);
+int he_i8_layer_destroy(he_i8_layer* layer);
+int he_i8_workspace_bytes(const he_i8_layer* layer, uint32_t limbs, uint32_t flags, size_t* bytes);
+int he_ct_i8_mac(he_ctx* ctx, const he_i8_layer* layer, uint32_t limbs, const uint64_t* ct_in, const uint64_t* token_scale,
+                 const uint64_t* bias, uint64_t* ct_out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Packed 32-bit storage: the paper's optimisation for moduli of at most 32 bits (Sec.
  * "Ciphertext-plaintext Multiplication": BarrettReduction64, Alg. 6, and Alg. 8) with the residues
- * stored as uint32, half the bytes of the 64-bit form.  The calls below mirror he_ct_pt_mac,
+ * stored as uint32, half the bytes of the 64-bit form.  The calls below mirror he_ct_pt_mac, he_ct_i8_mac,
  * he_ct_pt_add, he_rescale, he_ntt_fwd and he_ntt_inv on tensors dev uint32 [ct][2][limbs][N] and
  * compute the same residues.  Every limb of the level must be below 2^30 (the lazy 32-bit butterflies
  * need 4q < 2^32), else HE_ERR_MODULUS.  Scalar plaintexts and biases stay uint64 [n][limbs], as
@@ -236,6 +266,7 @@ int he_ct_square_relin(he_ctx* ctx, uint32_t limbs, const uint64_t* ct_in, uint3
  *
  * he_pack32 / he_unpack32 convert `count` residues between the two forms (dev pointers, which must
  * not overlap; values of at least 2^32 lose their high word in he_pack32).
+ * he_ct_i8_mac32 takes the same layer as he_ct_i8_mac, token_scale dev uint32 [limbs][N].
  * he_ct_pt_mac32 takes the same plan and the same workspace size (he_plan_workspace_bytes) as
  * he_ct_pt_mac, and the same flags; the no-overlap rule of he_ct_pt_mac applies.
  */
@@ -244,6 +275,8 @@ int he_unpack32(he_ctx* ctx, const uint32_t* in, uint64_t* out, size_t count, vo
 int he_ct_pt_mac32(he_ctx* ctx, const he_plan* plan, uint32_t limbs, const uint32_t* ct_in, const void* pt,
                    int pt_kind, const uint64_t* bias, uint32_t* ct_out, uint32_t flags, void* workspace,
                    size_t workspace_bytes, void* stream);
+int he_ct_i8_mac32(he_ctx* ctx, const he_i8_layer* layer, uint32_t limbs, const uint32_t* ct_in, const uint32_t* token_scale,
+                   const uint64_t* bias, uint32_t* ct_out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 int he_ct_pt_add32(he_ctx* ctx, uint32_t limbs, uint32_t* ct, uint32_t n, const void* pt, int pt_kind,
                    void* stream);
 int he_rescale32(he_ctx* ctx, uint32_t limbs, const uint32_t* in, uint32_t* out, uint32_t n, void* stream);

@@ -736,10 +736,9 @@ static int build_plan(he_plan* p, const u32* off, const u32* term_ct, const u32*
     return HE_OK;
 }
 
-int he_plan_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt, const uint32_t* off,
-                   const uint32_t* term_ct, const uint32_t* term_pt, he_plan** out) {
-    if (!out) return HE_ERR_ARG;
-    *out = nullptr;
+// The arrays of a plan or an int8 layer
+static int check_plan(const he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt, const uint32_t* off, const uint32_t* term_ct,
+                      const uint32_t* term_pt) {
     if (!ctx || !off) return HE_ERR_ARG;
     if (off[0] != 0) return HE_ERR_RANGE;
     for (u32 o = 0; o < n_out; ++o)
@@ -748,8 +747,17 @@ int he_plan_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt, co
     if (n_terms && (!term_ct || !term_pt)) return HE_ERR_ARG;
     for (u32 t = 0; t < n_terms; ++t)
         if (term_ct[t] >= n_in || term_pt[t] >= n_pt) return HE_ERR_RANGE;
-    int rc = need_device(ctx);
+    return HE_OK;
+}
+
+int he_plan_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt, const uint32_t* off,
+                   const uint32_t* term_ct, const uint32_t* term_pt, he_plan** out) {
+    if (!out) return HE_ERR_ARG;
+    *out = nullptr;
+    int rc = check_plan(ctx, n_in, n_out, n_pt, off, term_ct, term_pt);
     if (rc != HE_OK) return rc;
+    const u32 n_terms = off[n_out];
+    if ((rc = need_device(ctx)) != HE_OK) return rc;
     he_plan* p = new (std::nothrow) he_plan();  // (all pointers null)
     if (!p) return HE_ERR_ARG;
     p->ctx = ctx;
@@ -987,6 +995,109 @@ int he_ct_square_relin(he_ctx* ctx, uint32_t limbs, const uint64_t* ct_in, uint3
     return launch_square_relin(ctx, limbs, ct_in, n, evk, ct_out, workspace, (hipStream_t)stream);
 }
 
+// ---- int8 layers
+
+int he_i8_layer_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt, const uint32_t* off, const uint32_t* term_ct,
+                       const uint32_t* term_pt, const int8_t* weights, const double* channel_scale, double scale, he_i8_layer** out) {
+    if (!out) return HE_ERR_ARG;
+    *out = nullptr;
+    int rc = check_plan(ctx, n_in, n_out, n_pt, off, term_ct, term_pt);
+    if (rc != HE_OK) return rc;
+    if (off[n_out] && !weights) return HE_ERR_ARG;
+    for (u32 o = 0; o < n_out; ++o)
+        if (off[o + 1] - off[o] > I8_MAX_TERMS) return HE_ERR_RANGE;
+    he_i8_layer* l = nullptr;
+    try {
+        std::vector<u64> residues;
+        if (channel_scale) {
+            residues.resize((size_t)n_out * ctx->L);
+            for (u32 o = 0; o < n_out; ++o)
+                if (!encode_one(channel_scale[o], scale, ctx->limbs.c, ctx->L, residues.data() + (size_t)o * ctx->L)) return HE_ERR_ARG;
+        }
+        if ((rc = need_device(ctx)) != HE_OK) return rc;
+        l = new he_i8_layer();  // (all pointers null)
+        l->ctx = ctx;
+        l->device = ctx->device;
+        l->n_in = n_in; l->n_out = n_out; l->n_terms = off[n_out];
+        I8Host h;
+        build_i8_layer(ctx, off, term_ct, term_pt, weights, channel_scale ? residues.data() : nullptr, l, h);
+        if (upload(&l->groups_dev, h.groups.data(), h.groups.size()) != HE_OK || upload(&l->lists_dev, h.lists.data(), h.lists.size()) != HE_OK ||
+            upload(&l->table_dev, h.table.data(), h.table.size()) != HE_OK || upload(&l->mult_dev, h.mult.data(), h.mult.size()) != HE_OK ||
+            upload(&l->addend_dev, h.addend.data(), h.addend.size()) != HE_OK ||
+            upload(&l->addend32_dev, h.addend32.data(), h.addend32.size()) != HE_OK)
+            rc = HE_ERR_DEVICE;
+    } catch (const std::bad_alloc&) {
+        rc = HE_ERR_RANGE;
+    }
+    if (rc != HE_OK) {
+        if (l) he_i8_layer_destroy(l);
+        return rc;
+    }
+    *out = l;
+    return HE_OK;
+}
+
+int he_i8_layer_destroy(he_i8_layer* l) {
+    if (!l) return HE_ERR_ARG;
+    if (l->device >= 0 && hipSetDevice(l->device) == hipSuccess) {
+        void* bufs[] = {l->groups_dev, l->lists_dev, l->table_dev, l->mult_dev, l->addend_dev, l->addend32_dev};
+        for (void* b : bufs)
+            if (b) (void)hipFree(b);
+    }
+    (void)hipGetLastError();
+    delete l;
+    return HE_OK;
+}
+
+int he_i8_workspace_bytes(const he_i8_layer* layer, uint32_t limbs, uint32_t flags, size_t* bytes) {
+    if (!layer || !bytes) return HE_ERR_ARG;
+    if (flags & ~(HE_RESCALE | HE_ACCUMULATE)) return HE_ERR_ARG;
+    if ((flags & HE_RESCALE) && (flags & HE_ACCUMULATE)) return HE_ERR_ARG;
+    int rc = check_level(layer->ctx, limbs, (flags & HE_RESCALE) ? 2 : 1);
+    if (rc != HE_OK) return rc;
+    *bytes = (flags & HE_RESCALE) ? align256((size_t)layer->n_out * 2 * limbs * layer->ctx->N * sizeof(u64)) : 0;
+    return HE_OK;
+}
+
+// What he_ct_i8_mac and he_ct_i8_mac32 have in common: the checks of a call (word: bytes of a residue; *work: whether there is anything to do).
+static int check_i8_call(he_ctx* ctx, const he_i8_layer* l, uint32_t limbs, const void* ct_in, const void* token_scale, const uint64_t* bias,
+                         const void* ct_out, uint32_t flags, const void* workspace, size_t workspace_bytes, size_t word, bool* work) {
+    *work = false;
+    if (!ctx || !l || l->ctx != ctx) return HE_ERR_ARG;
+    size_t need = 0;
+    int rc = he_i8_workspace_bytes(l, limbs, flags, &need);
+    if (rc != HE_OK) return rc;
+    if (l->n_out == 0) return HE_OK;
+    if (!ct_out || (l->n_terms && !ct_in)) return HE_ERR_ARG;
+    if (need && (!workspace || workspace_bytes < need)) return HE_ERR_WORKSPACE;
+    const size_t row = (size_t)ctx->N * word;
+    const size_t out_bytes = (size_t)l->n_out * 2 * ((flags & HE_RESCALE) ? limbs - 1 : limbs) * row;
+    const size_t in_bytes = (size_t)l->n_in * 2 * limbs * row, token_bytes = limbs * row, bias_bytes = (size_t)l->n_out * limbs * sizeof(u64);
+    if (overlaps(ct_out, out_bytes, ct_in, in_bytes) || overlaps(ct_out, out_bytes, token_scale, token_bytes) ||
+        overlaps(ct_out, out_bytes, bias, bias_bytes) || overlaps(ct_out, out_bytes, workspace, need) ||
+        overlaps(workspace, need, ct_in, in_bytes) || overlaps(workspace, need, token_scale, token_bytes) ||
+        overlaps(workspace, need, bias, bias_bytes))
+        return HE_ERR_ARG;
+    if ((rc = check_i8_launch(ctx, l, limbs, word == sizeof(u32))) != HE_OK) return rc;
+    if ((flags & HE_RESCALE) && l->n_out > 0x3FFFFFFFu) return HE_ERR_RANGE;
+    *work = true;
+    return need_device(ctx);
+}
+
+int he_ct_i8_mac(he_ctx* ctx, const he_i8_layer* layer, uint32_t limbs, const uint64_t* ct_in, const uint64_t* token_scale,
+                 const uint64_t* bias, uint64_t* ct_out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+    bool work;
+    int rc = check_i8_call(ctx, layer, limbs, ct_in, token_scale, bias, ct_out, flags, workspace, workspace_bytes, sizeof(u64), &work);
+    if (rc != HE_OK || !work) return rc;
+    hipStream_t s = (hipStream_t)stream;
+    if (flags & HE_RESCALE) {
+        u64* acc = (u64*)workspace;
+        if ((rc = launch_i8(ctx, layer, limbs, ct_in, token_scale, bias, acc, 0, s)) != HE_OK) return rc;
+        return launch_rescale(ctx, limbs, acc, ct_out, layer->n_out, s);
+    }
+    return launch_i8(ctx, layer, limbs, ct_in, token_scale, bias, ct_out, (flags & HE_ACCUMULATE) ? 1u : 0u, s);
+}
+
 // ---- packed 32-bit storage
 
 // every limb of the level must have a 32-bit form
@@ -1055,6 +1166,23 @@ int he_ct_pt_mac32(he_ctx* ctx, const he_plan* plan, uint32_t limbs, const uint3
         return launch_rescale32(ctx, limbs, acc, ct_out, plan->n_out, s);
     }
     return launch_mac32(ctx, plan, limbs, ct_in, pt, pt_kind, bias, ct_out, workspace, (flags & HE_ACCUMULATE) ? 1u : 0u, s);
+}
+
+int he_ct_i8_mac32(he_ctx* ctx, const he_i8_layer* layer, uint32_t limbs, const uint32_t* ct_in, const uint32_t* token_scale,
+                   const uint64_t* bias, uint32_t* ct_out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!ctx) return HE_ERR_ARG;
+    int rc = check_level32(ctx, limbs, (flags & HE_RESCALE) ? 2 : 1);
+    if (rc != HE_OK) return rc;
+    bool work;
+    rc = check_i8_call(ctx, layer, limbs, ct_in, token_scale, bias, ct_out, flags, workspace, workspace_bytes, sizeof(u32), &work);
+    if (rc != HE_OK || !work) return rc;
+    hipStream_t s = (hipStream_t)stream;
+    if (flags & HE_RESCALE) {
+        u32* acc = (u32*)workspace;
+        if ((rc = launch_i8_32(ctx, layer, limbs, ct_in, token_scale, bias, acc, 0, s)) != HE_OK) return rc;
+        return launch_rescale32(ctx, limbs, acc, ct_out, layer->n_out, s);
+    }
+    return launch_i8_32(ctx, layer, limbs, ct_in, token_scale, bias, ct_out, (flags & HE_ACCUMULATE) ? 1u : 0u, s);
 }
 
 int he_ct_pt_add32(he_ctx* ctx, uint32_t limbs, uint32_t* ct, uint32_t n, const void* pt, int pt_kind, void* stream) {

@@ -150,6 +150,47 @@ struct he_plan {
     u32* term_pt_dev;
 };
 
+// ---- int8 layers (he_i8.hip)
+constexpr u32 I8_CLASSES = 4;          // groups of up to 32, 64, 96 and 128 outputs
+constexpr u32 I8_MAX_TERMS = 131071;   // of an output: sums of so many products of at most 2^14 stay below 2^31
+// Outputs that read the same ciphertexts in the same order.
+struct I8Group {
+    u32 out0, count;
+    u32 n_terms;   // of each output
+    u32 list;      // where the ciphertexts of the terms start in he_i8_layer::lists_dev, in blocks of 32 terms
+    u32 table;     // where the weights start in he_i8_layer::table_dev, in tiles of 1024 bytes
+    u32 pad[3];
+};
+// What one half of an output's sum is multiplied by: a residue and its Shoup companion.
+struct I8Mult {
+    u64 w, w_shoup;
+};
+// Per limb: the digits of a residue that each of two wavefronts takes (2, 3 or 4).
+struct I8Nd {
+    u32 nd[HE_MAX_LIMBS];
+};
+struct he_i8_layer {
+    he_ctx* ctx;
+    int device;
+    u32 n_in, n_out, n_terms;
+    u32 class_begin[I8_CLASSES + 1];  // groups sorted by the tiles of 32 outputs that they take
+    I8Nd nd;
+    I8Group* groups_dev;
+    u32* lists_dev;    // the groups' ciphertexts, padded to blocks of 32 with the last one
+    int8_t* table_dev; // the weights as the matrix instructions take them, shared by groups with the same ones
+    I8Mult* mult_dev;  // [L][n_out][2]
+    u64* addend_dev;   // [L][n_out]: what the offsets of a sum leave to add, times the channel's scale
+    u64* addend32_dev; // ... in packed storage
+};
+// What of a layer is built on the host.
+struct I8Host {
+    std::vector<I8Group> groups;
+    std::vector<u32> lists;
+    std::vector<int8_t> table;
+    std::vector<I8Mult> mult;
+    std::vector<u64> addend, addend32;
+};
+
 #define HE_HIP(call)                                   \
     do {                                               \
         if ((call) != hipSuccess) {                    \
@@ -240,3 +281,11 @@ int launch_ntt32(he_ctx* ctx, u32 limbs, u32* data, u32 rows, bool inverse, hipS
 int launch_rescale32(he_ctx* ctx, u32 limbs, const u32* in, u32* out, u32 n, hipStream_t s);
 int launch_encode_vector(he_ctx* ctx, u32 limbs, const double* slots, u32 n, double scale, u64* out, hipStream_t s);
 int launch_decode_vector(he_ctx* ctx, u32 limbs, const u64* coef, u32 n, double scale, double* slots, hipStream_t s);
+// int8 layers (he_i8.hip); scale: host [n_out][L] residues or null
+void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const u32* term_pt, const int8_t* weights, const u64* scale,
+                    he_i8_layer* l, I8Host& h);
+int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed);
+int launch_i8(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const u64* ct_in, const u64* token, const u64* bias, u64* out, u32 accumulate,
+              hipStream_t s);
+int launch_i8_32(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const u32* ct_in, const u32* token, const u64* bias, u32* out, u32 accumulate,
+                 hipStream_t s);

@@ -34,6 +34,7 @@ EXPORTS = [
     "he_ntt_fwd", "he_ntt_inv", "he_check_reduced", "he_host_mulmod", "he_host_reduce128", "he_host_shoup_mulmod", "he_host_shoup_lazy",
     "he_host_mac_accumulate", "he_host_mac_accumulate_add", "he_host_mac_accumulate_lazy", "he_test_mac_for_rescale", "he_measure_rate",
     "he_host_barrett64", "he_host_shoup32", "he_host_mac_digits", "he_host_digit_reduce", "he_test_mac_groups_per_workgroup", "he_test_mac_form", "he_host_ntt_forward_fp64", "he_host_ntt_expand_fp64", "he_host_ntt_inverse_fp64", "he_test_integer_transforms", "he_square_relin_workspace_bytes", "he_ct_square_relin", "he_pack32", "he_unpack32", "he_ct_pt_mac32", "he_ct_pt_add32", "he_rescale32", "he_ntt_fwd32", "he_ntt_inv32",
+    "he_i8_layer_create", "he_i8_layer_destroy", "he_i8_workspace_bytes", "he_ct_i8_mac", "he_ct_i8_mac32",
 ]
 
 _lib = None
@@ -102,6 +103,11 @@ def lib():
         "he_rescale32": (i32, [vp, u32, vp, vp, u32, vp]),
         "he_ntt_fwd32": (i32, [vp, u32, vp, u32, vp]),
         "he_ntt_inv32": (i32, [vp, u32, vp, u32, vp]),
+        "he_i8_layer_create": (i32, [vp, u32, u32, u32, vp, vp, vp, vp, vp, dbl, pp]),
+        "he_i8_layer_destroy": (i32, [vp]),
+        "he_i8_workspace_bytes": (i32, [vp, u32, u32, ctypes.POINTER(sz)]),
+        "he_ct_i8_mac": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
+        "he_ct_i8_mac32": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
@@ -344,6 +350,41 @@ class Context:
                                          _dev_ptr(bias, "bias"), _dev_ptr(out, "ct_out"), flags, _stream()), "he_ct_pt_mac_static")
         return out
 
+    # -- layers of 8-bit integer weights
+    def i8_layer(self, n_in: int, n_out: int, n_pt: int, off, term_ct, term_pt, weights, channel_scale=None, scale: float = 1.0) -> "I8Layer":
+        return I8Layer(self, n_in, n_out, n_pt, off, term_ct, term_pt, weights, channel_scale, scale)
+
+    def _i8_mac(self, name, dtype, layer, ct_in, token_scale, bias, flags, out, workspace):
+        import torch
+        limbs = ct_in.shape[2]
+        assert ct_in.dtype == dtype and tuple(ct_in.shape) == (layer.n_in, 2, limbs, self.N)
+        assert token_scale is None or (token_scale.dtype == dtype and tuple(token_scale.shape) == (limbs, self.N))
+        assert bias is None or (bias.dtype == torch.int64 and tuple(bias.shape) == (layer.n_out, limbs))
+        out_limbs = limbs - 1 if flags & RESCALE else limbs
+        if out is None:
+            assert not flags & ACCUMULATE, "HE_ACCUMULATE adds to an output the caller provides"
+            out = torch.empty((layer.n_out, 2, out_limbs, self.N), dtype=dtype, device=ct_in.device)
+        assert out.dtype == dtype and tuple(out.shape) == (layer.n_out, 2, out_limbs, self.N)
+        if workspace is None:
+            need = layer.workspace_bytes(limbs, flags)
+            workspace = torch.empty(need, dtype=torch.uint8, device=ct_in.device) if need else None
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        _check(getattr(lib(), name)(self._h, layer._h, limbs, _dev_ptr(ct_in, "ct_in"), _dev_ptr(token_scale, "token_scale"),
+                                    _dev_ptr(bias, "bias"), _dev_ptr(out, "ct_out"), flags, _dev_ptr(workspace, "workspace"),
+                                    ws_bytes, _stream()), name)
+        return out
+
+    def ct_i8_mac(self, layer: "I8Layer", ct_in, token_scale=None, bias=None, flags: int = 0, out=None, workspace=None):
+        """ct_in [n_in][2][limbs][N] -> out [n_out][2][limbs or limbs-1][N]; token_scale [limbs][N] (NTT form), bias [n_out][limbs]
+        (he_ct_i8_mac)."""
+        import torch
+        return self._i8_mac("he_ct_i8_mac", torch.int64, layer, ct_in, token_scale, bias, flags, out, workspace)
+
+    def ct_i8_mac32(self, layer: "I8Layer", ct_in, token_scale=None, bias=None, flags: int = 0, out=None, workspace=None):
+        """The same on packed residues: ct_in, token_scale and out int32, bias int64 (he_ct_i8_mac32)."""
+        import torch
+        return self._i8_mac("he_ct_i8_mac32", torch.int32, layer, ct_in, token_scale, bias, flags, out, workspace)
+
     # -- the x^2 activation: square + relinearise, the context's last limb being the special prime
     def square_relin_workspace_bytes(self, limbs: int, n: int) -> int:
         b = ctypes.c_size_t()
@@ -474,6 +515,43 @@ class Plan:
     def close(self):
         if getattr(self, "_h", None):
             lib().he_plan_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class I8Layer:
+    """he_i8_layer: out[o] = s_o * (sum over t in [off[o], off[o+1]) of weights[term_pt[t]] * ct_in[term_ct[t]]), s_o the encoding of
+    channel_scale[o] at `scale` (1 without channel_scale); weights int8 [n_pt], channel_scale float64 [n_out], both host arrays."""
+
+    def __init__(self, ctx: Context, n_in: int, n_out: int, n_pt: int, off, term_ct, term_pt, weights, channel_scale=None, scale: float = 1.0):
+        self.ctx, self.n_in, self.n_out, self.n_pt = ctx, int(n_in), int(n_out), int(n_pt)
+        off, term_ct, term_pt = _np32(off), _np32(term_ct), _np32(term_pt)
+        weights = np.ascontiguousarray(weights)
+        assert weights.dtype == np.int8 and weights.shape == (self.n_pt,)
+        assert off.size == self.n_out + 1 and term_ct.size == term_pt.size
+        if channel_scale is not None:
+            channel_scale = np.ascontiguousarray(channel_scale, dtype=np.float64)
+            assert channel_scale.shape == (self.n_out,)
+        h = ctypes.c_void_p()
+        _check(lib().he_i8_layer_create(ctx._h, self.n_in, self.n_out, self.n_pt, off.ctypes.data, term_ct.ctypes.data,
+                                        term_pt.ctypes.data, weights.ctypes.data,
+                                        None if channel_scale is None else channel_scale.ctypes.data, float(scale), ctypes.byref(h)),
+               "he_i8_layer_create")
+        self._h = h
+
+    def workspace_bytes(self, limbs: int, flags: int) -> int:
+        b = ctypes.c_size_t()
+        _check(lib().he_i8_workspace_bytes(self._h, limbs, flags, ctypes.byref(b)), "he_i8_workspace_bytes")
+        return int(b.value)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().he_i8_layer_destroy(self._h)
             self._h = None
 
     def __del__(self):
