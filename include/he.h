@@ -120,6 +120,31 @@ int he_decode_vector(he_ctx* ctx, const uint64_t* poly, size_t n, double scale, 
                      double* slots, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Sampling, what a client does with decoded logits: one token per row of slots dev [n][N/2][2] double, as he_decode_vector
+ * writes them, from n ciphertexts that hold the logits of n classes (or of a vocabulary of n tokens), 1 <= n <= 32768 (HE_ERR_RANGE).
+ * The rows are the first n_slots slots' real parts (HE_SLOTS_REAL: row s), or real and imaginary parts (HE_SLOTS_COMPLEX, "Complex packing":
+ * rows 2s and 2s + 1).  All other arrays are dev [rows]; each filter may be NULL (off for all rows):
+ *   temperature  T > 0; a row whose T is not above zero takes the largest logit (the lowest index of several); NULL: 1
+ *   top_k        uint32: the k tokens of the largest weights; 0, or at least n: off
+ *   top_p        of these the fewest, in descending order, whose weights sum to p times their sum or more; p >= 1 or NaN: off;
+ *                p <= 0: one token
+ *   min_p        of these the ones of at least min_p times the largest weight; <= 0 or NaN: off; the largest always stays
+ *   uniform      u in [0, 1): the token is the first, in the order of the indices, at which the running sum of the kept weights exceeds
+ *                floor(u * their sum) (values outside the range, NaN as 0, are taken to its ends)
+ * The weights are whole numbers, w_v = round(2^47 * exp((l_v - max) * (1 / T))) and 2^47 where l_v is the row's maximum; tokens of equal
+ * weight are in the order of their indices.  All sums are exact, so a row's token depends on nothing but its inputs.  A NaN
+ * or -infinity among the logits is never taken; a row that has nothing else gets token -1.
+ * tokens: dev int32 [rows].  log_prob: dev double [rows] or NULL: the logarithm of the token's weight (not rounded) over the sum of
+ * the kept ones; 0 where the largest logit was taken without sampling, -infinity for token -1.  The outputs must not overlap the inputs nor each other
+ * (HE_ERR_ARG).  One kernel on `stream`.
+ */
+#define HE_SLOTS_REAL 1
+#define HE_SLOTS_COMPLEX 2
+int he_sample_slots(he_ctx* ctx, const double* slots, uint32_t n, uint32_t n_slots, uint32_t parts, const double* temperature,
+                    const uint32_t* top_k, const double* top_p, const double* min_p, const double* uniform, int32_t* tokens, double* log_prob,
+                    void* stream);
+
+/*
  * A MAC plan (Sec. "Lazy Rescaling": an FC or Convolution output is a sum over the inner
  * dimension / window):  out[o] = sum over t in [off[o], off[o+1]) of
  * ct_in[term_ct[t]] * pt[term_pt[t]].  All three arrays are host memory and are copied;

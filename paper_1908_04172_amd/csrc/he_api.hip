@@ -612,6 +612,26 @@ int he_decode_vector(he_ctx* ctx, const uint64_t* poly, size_t n, double scale, 
     return launch_decode_vector(ctx, limbs, (const u64*)workspace, (u32)n, scale, slots, s);
 }
 
+int he_sample_slots(he_ctx* ctx, const double* slots, uint32_t n, uint32_t n_slots, uint32_t parts, const double* temperature,
+                    const uint32_t* top_k, const double* top_p, const double* min_p, const double* uniform, int32_t* tokens, double* log_prob,
+                    void* stream) {
+    if (!ctx || n == 0 || (parts != HE_SLOTS_REAL && parts != HE_SLOTS_COMPLEX)) return HE_ERR_ARG;
+    if (n > SAMPLE_MAX_TOKENS || n_slots > ctx->N / 2) return HE_ERR_RANGE;
+    if (n_slots == 0) return HE_OK;
+    if (!slots || !uniform || !tokens) return HE_ERR_ARG;
+    {
+        const size_t rows = (size_t)n_slots * parts, d = rows * sizeof(double), w = rows * sizeof(u32);
+        struct { const void* p; size_t bytes; } in[] = {{slots, (size_t)n * ctx->N * sizeof(double)}, {temperature, d}, {top_k, w}, {top_p, d},
+                                                        {min_p, d}, {uniform, d}};
+        for (const auto& i : in)
+            if (overlaps(tokens, w, i.p, i.bytes) || overlaps(log_prob, d, i.p, i.bytes)) return HE_ERR_ARG;
+        if (overlaps(tokens, w, log_prob, d)) return HE_ERR_ARG;
+    }
+    int rc = need_device(ctx);
+    if (rc != HE_OK) return rc;
+    return launch_sample(ctx, slots, n, n_slots, parts, temperature, top_k, top_p, min_p, uniform, tokens, log_prob, (hipStream_t)stream);
+}
+
 int he_encode_scalar_host(const he_ctx* ctx, const double* values, size_t n, double scale, uint32_t limbs,
                           uint64_t* out) {
     int rc = check_level(ctx, limbs, 1);

@@ -289,3 +289,7 @@ int launch_i8(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const u64* ct_in, co
               hipStream_t s);
 int launch_i8_32(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const u32* ct_in, const u32* token, const u64* bias, u32* out, u32 accumulate,
                  hipStream_t s);
+// sampling from decoded slots (he_sample.hip)
+constexpr u32 SAMPLE_MAX_TOKENS = 32768;
+int launch_sample(he_ctx* ctx, const double* slots, u32 n, u32 n_slots, u32 parts, const double* temperature, const u32* top_k, const double* top_p,
+                  const double* min_p, const double* uniform, int32_t* tokens, double* log_prob, hipStream_t s);

@@ -22,6 +22,8 @@ PT_SCALAR = 0
 PT_POLY = 1
 RESCALE = 1
 ACCUMULATE = 2
+SLOTS_REAL = 1
+SLOTS_COMPLEX = 2
 STATIC_SCRATCH_BYTES = 32 << 20
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -35,6 +37,7 @@ EXPORTS = [
     "he_host_mac_accumulate", "he_host_mac_accumulate_add", "he_host_mac_accumulate_lazy", "he_test_mac_for_rescale", "he_measure_rate",
     "he_host_barrett64", "he_host_shoup32", "he_host_mac_digits", "he_host_digit_reduce", "he_test_mac_groups_per_workgroup", "he_test_mac_form", "he_host_ntt_forward_fp64", "he_host_ntt_expand_fp64", "he_host_ntt_inverse_fp64", "he_test_integer_transforms", "he_square_relin_workspace_bytes", "he_ct_square_relin", "he_pack32", "he_unpack32", "he_ct_pt_mac32", "he_ct_pt_add32", "he_rescale32", "he_ntt_fwd32", "he_ntt_inv32",
     "he_i8_layer_create", "he_i8_layer_destroy", "he_i8_workspace_bytes", "he_ct_i8_mac", "he_ct_i8_mac32",
+    "he_sample_slots",
 ]
 
 _lib = None
@@ -107,6 +110,7 @@ def lib():
         "he_i8_layer_destroy": (i32, [vp]),
         "he_i8_workspace_bytes": (i32, [vp, u32, u32, ctypes.POINTER(sz)]),
         "he_ct_i8_mac": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
+        "he_sample_slots": (i32, [vp, vp, u32, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp]),
         "he_ct_i8_mac32": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
     }
     for name, (res, args) in sigs.items():
@@ -252,6 +256,28 @@ class Context:
         _check(lib().he_decode_vector(self._h, _dev_ptr(poly, "poly"), n, float(scale), limbs, _dev_ptr(out, "slots"),
                                       _dev_ptr(workspace, "workspace"), workspace.numel(), _stream()), "he_decode_vector")
         return out
+
+    def sample_slots(self, slots, uniform, parts: int = SLOTS_REAL, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+                     log_prob=None):
+        """slots: CUDA complex128 tensor [n][N/2]; uniform and the other floats CUDA float64 tensors [rows], top_k int32 [rows], where rows is
+        `parts` times the number of leading slots to read -> (tokens int32 [rows], log_prob float64 [rows]) (he_sample_slots)."""
+        import torch
+        n, half = slots.shape
+        rows = uniform.numel()
+        assert slots.dtype == torch.complex128 and half == self.N // 2 and rows % parts == 0
+        for t in (uniform, temperature, top_p, min_p, log_prob):
+            assert t is None or (t.dtype == torch.float64 and tuple(t.shape) == (rows,))
+        assert top_k is None or (top_k.dtype == torch.int32 and tuple(top_k.shape) == (rows,))
+        if out is None:
+            out = torch.empty(rows, dtype=torch.int32, device=slots.device)
+        if log_prob is None:
+            log_prob = torch.empty(rows, dtype=torch.float64, device=slots.device)
+        assert out.dtype == torch.int32 and tuple(out.shape) == (rows,)
+        _check(lib().he_sample_slots(self._h, _dev_ptr(slots, "slots"), n, rows // parts, parts, _dev_ptr(temperature, "temperature"),
+                                     _dev_ptr(top_k, "top_k"), _dev_ptr(top_p, "top_p"), _dev_ptr(min_p, "min_p"),
+                                     _dev_ptr(uniform, "uniform"), _dev_ptr(out, "tokens"), _dev_ptr(log_prob, "log_prob"), _stream()),
+               "he_sample_slots")
+        return out, log_prob
 
     # -- Alg. 3 / 4
     def ct_pt_add(self, ct, pt, pt_kind: int, limbs: Optional[int] = None):
