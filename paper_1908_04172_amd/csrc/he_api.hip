@@ -1042,9 +1042,8 @@ int he_i8_layer_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt
         I8Host h;
         build_i8_layer(ctx, off, term_ct, term_pt, weights, channel_scale ? residues.data() : nullptr, l, h);
         if (upload(&l->groups_dev, h.groups.data(), h.groups.size()) != HE_OK || upload(&l->lists_dev, h.lists.data(), h.lists.size()) != HE_OK ||
-            upload(&l->table_dev, h.table.data(), h.table.size()) != HE_OK || upload(&l->mult_dev, h.mult.data(), h.mult.size()) != HE_OK ||
-            upload(&l->addend_dev, h.addend.data(), h.addend.size()) != HE_OK ||
-            upload(&l->addend32_dev, h.addend32.data(), h.addend32.size()) != HE_OK)
+            upload(&l->table_dev, h.table.data(), h.table.size()) != HE_OK || upload(&l->channels_dev, h.channels.data(), h.channels.size()) != HE_OK ||
+            upload(&l->channels32_dev, h.channels32.data(), h.channels32.size()) != HE_OK)
             rc = HE_ERR_DEVICE;
     } catch (const std::bad_alloc&) {
         rc = HE_ERR_RANGE;
@@ -1060,7 +1059,7 @@ int he_i8_layer_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt
 int he_i8_layer_destroy(he_i8_layer* l) {
     if (!l) return HE_ERR_ARG;
     if (l->device >= 0 && hipSetDevice(l->device) == hipSuccess) {
-        void* bufs[] = {l->groups_dev, l->lists_dev, l->table_dev, l->mult_dev, l->addend_dev, l->addend32_dev};
+        void* bufs[] = {l->groups_dev, l->lists_dev, l->table_dev, l->channels_dev, l->channels32_dev};
         for (void* b : bufs)
             if (b) (void)hipFree(b);
     }

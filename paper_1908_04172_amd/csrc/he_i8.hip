@@ -9,14 +9,16 @@
 // flipped, and what that leaves out, 128 sum_d 256^d sum_t w_t, is a constant of the output.
 //
 // v_mfma_i32_32x32x32_i8 takes 32 terms times 32 outputs times 32 slots of one digit.  A lane's share of the input operand is one byte of 16
-// terms at one slot: it loads four bytes of each of the 16 residues and transposes them in registers (4 x 4 bytes: eight byte
-// permutations).  A wavefront takes half of the digits (bytes 0 .. ND-1 or ND .. 2 ND-1, ND = 2, 3 or 4 by the modulus), so
-// that up to 128 outputs times 32 slots of sums fit its registers and the inputs are read once for up to 128 outputs; two
-// wavefronts share a slot, and meet at the end to add their parts.  Residues in packed storage are four bytes: one wavefront.
+// terms at one slot: it loads the bytes of each of the 16 residues and transposes them in registers (4 x 4 bytes: eight byte
+// permutations).  The digits go in two halves, bytes 0 .. ND-1 and ND .. 2 ND-1 (ND = 2, 3 or 4 by the modulus), in one of two forms:
+//  - groups of up to 32 outputs (convolutions, narrow layers): a wavefront takes both halves of 32 slots and runs through several
+//    groups, the inputs of the next block of terms in flight; wavefronts never meet;
+//  - larger ones: a wavefront takes one half, which leaves room for the sums of up to 128 outputs, so that the inputs are read
+//    once for so many; the two wavefronts of a slot exchange half of their results at the end.
+// Residues in packed storage are taken two at a time as one of eight bytes (first form), or one half alone (second).
 //
-// The end of an output: y = sum of its digits' sums, |y| < 2^55.1, plus 2^56, is multiplied by s_o (the upper half's by s_o 256^ND) with a
-// Shoup product, which reduces it and applies the channel's scale at once; the offsets, the flipped bits' constant and s_o are
-// one constant per output and limb.
+// The end of an output: with y0, y1 the halves' sums, |y| < 2^55.1, each plus 2^56, r = y0 + (y1 256^ND mod q) is one Shoup product, and
+// r s_o another, whose result is below 2q; what the offsets, the flipped bits and s_o leave to add is a constant of the output and limb.
 #include <string.h>
 
 #include <algorithm>
@@ -29,32 +31,45 @@ namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
-typedef u32 u32_any __attribute__((aligned(1)));  // four bytes of a residue, at any byte
+typedef u32 u32_any __attribute__((aligned(1)));                            // four bytes of a residue, at any byte
+typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 constexpr u32 THREADS = 256, WAVES = THREADS / 64;
-constexpr int OFFSET_BITS = 56;  // what makes a part of a sum positive
+constexpr int OFFSET_BITS = 56;      // what makes a half of a sum positive
+constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most
+constexpr u64 MIN_WORKGROUPS = 2048; // ... while the launch keeps at least this many workgroups
 
+// slots of a workgroup: first form (32 units of eight bytes per wavefront), second form (two wavefronts per slot, or one)
 template <typename V>
-struct Form {
-    static constexpr u32 PARTS = sizeof(V) / 4;               // wavefronts that share a slot
-    static constexpr u32 SLOTS = 32 * WAVES / PARTS;          // slots of a workgroup
-};
+__host__ __device__ constexpr u32 whole_slots() { return 32 * WAVES * 8 / sizeof(V); }
+template <typename V>
+__host__ __device__ constexpr u32 split_slots() { return 32 * WAVES * 4 / sizeof(V); }
 
 template <typename V>
 struct I8Args {
     const I8Group* groups;
     const u32* lists;
     const v4i* table;
-    const I8Mult* mult;     // [limb][n_out][2]
-    const u64* addend;      // [limb][n_out]
+    const I8Channel* channels;  // [limb][n_out]
     const V* ct_in;
-    const V* token;         // [limbs][N] or null
-    const u64* bias;        // [n_out][limbs] or null
+    const V* token;             // [limbs][N] or null
+    const u64* bias;            // [n_out][limbs] or null
     V* out;
     u32 limbs, N, n_out;
-    u32 first, n_groups;
+    u32 first, n_groups;        // the class's groups
+    u32 run, runs;              // groups of a workgroup, runs of groups
     u32 accumulate;
 };
+
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {  // read-only, workgroup-uniform data: a scalar load
+    return *(const __attribute__((address_space(4))) T*)(p);
+}
+__device__ __forceinline__ I8Group load_group(const I8Group* p) {
+    typedef u32 u32x8 __attribute__((ext_vector_type(8)));
+    const u32x8 v = *(const __attribute__((address_space(4))) u32x8*)(p);
+    return I8Group{v[0], v[1], v[2], v[3], v[4], {0, 0, 0}};
+}
 
 // four bytes of four terms -> the same byte of the four terms, for the first ND bytes, as signed digits
 template <int ND>
@@ -76,9 +91,9 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // one is short by at most 2
 __device__ __forceinline__ u64 shoup_companion(u64 w, const LimbConst& c) {
     u64 e = w * c.ratio_hi + mul_hi64(w, c.ratio_lo);
-    u64 r = 0 - e * c.q;  // w * 2^64 - e * q, below 4q < 2^64
+    u64 r = 0 - e * c.q;  // w * 2^64 - e * q, below 3q < 2^64
 #pragma unroll
-    for (int i = 0; i < 3; i++) {
+    for (int i = 0; i < 2; i++) {
         const bool more = r >= c.q;
         e += more;
         r -= more ? c.q : 0;
@@ -86,16 +101,252 @@ __device__ __forceinline__ u64 shoup_companion(u64 w, const LimbConst& c) {
     return e;
 }
 
+// What the ends of all outputs of a row have in common.
+template <typename V>
+struct End {
+    u64 q, two_q;
+    I8Limb limb;
+    u64 tok[sizeof(V) == 8 ? 1 : 2], tok_shoup[sizeof(V) == 8 ? 1 : 2];  // the tokens of this lane's slots
+    bool has_token, has_bias, accumulate;
+    int32_t b8, b16, b24;     // 2^8, 2^16, 2^24 as data (multiplied by a literal they become shifts and additions)
+
+    // the sum of one half's digits, made positive
+    template <int ND>
+    __device__ __forceinline__ u64 half(int32_t s0, int32_t s1, int32_t s2, int32_t s3) const {
+        int64_t v = (int64_t)(1ull << OFFSET_BITS) + (int64_t)s0;
+        v = (int64_t)s1 * b8 + v;
+        if constexpr (ND > 2) v = (int64_t)s2 * b16 + v;
+        if constexpr (ND > 3) v = (int64_t)s3 * b24 + v;
+        return (u64)v;
+    }
+    // both halves -> what the channel's scale multiplies: any 64-bit value congruent to the sum
+    __device__ __forceinline__ u64 join(u64 y0, u64 y1) const {
+        const u64 up = limb.cheap ? shoup_mul_lazy4(y1, limb.shift, limb.shift_shoup, q) : shoup_mul_lazy(y1, limb.shift, limb.shift_shoup, q);
+        return y0 + up;  // below 4q + 2^57 for q < 2^61, else below 2q + 2^57
+    }
+    // the residue of an output
+    __device__ __forceinline__ u64 finish(u64 r, const I8Channel& ch, u64 bias, int k) const {
+        u64 v = shoup_mul_lazy(r, ch.s, ch.s_shoup, q) + ch.addend;  // below 3q
+        if (has_token) {
+            v = v >= two_q ? v - two_q : v;
+            v = shoup_mul_lazy(v, tok[k], tok_shoup[k], q);
+        }
+        v += bias;                                                   // below 4q
+        v = v >= two_q ? v - two_q : v;
+        return v >= q ? v - q : v;
+    }
+};
+
+template <typename V>
+__device__ __forceinline__ End<V> end_of(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb, u32 row, u32 slot) {
+    End<V> e;
+    e.q = c.q;
+    e.two_q = c.two_q;
+    e.limb = limb;
+    e.has_token = a.token != nullptr;
+    e.has_bias = a.bias != nullptr && !(row & 1);
+    e.accumulate = a.accumulate;
+    e.b8 = 1 << 8;
+    e.b16 = 1 << 16;
+    e.b24 = 1 << 24;
+    asm volatile("" : "+s"(e.b8), "+s"(e.b16), "+s"(e.b24));
+#pragma unroll
+    for (u32 k = 0; k < sizeof(e.tok) / sizeof(u64); k++) {
+        e.tok[k] = e.tok_shoup[k] = 0;
+        if (e.has_token) {
+            e.tok[k] = a.token[(size_t)(row >> 1) * a.N + slot + k];
+            e.tok_shoup[k] = shoup_companion(e.tok[k], c);
+        }
+    }
+    return e;
+}
+
+// An output's channel and bias, which the ends read from the LDS.
+struct Ends {
+    I8Channel channel;
+    u64 bias;
+};
+template <typename V>
+__device__ __forceinline__ Ends ends_of(const I8Args<V>& a, u32 row, u32 output) {
+    return Ends{a.channels[(size_t)(row >> 1) * a.n_out + output], a.bias && !(row & 1) ? a.bias[(size_t)output * a.limbs + (row >> 1)] : 0};
+}
+
+// ---------------------------------------------------------------------------------------------
+// First form: up to 32 outputs.
+
+struct Cursor {
+    u32 group, block, blocks;
+    u32 list, table;
+};
+template <typename V>
+__device__ __forceinline__ Cursor enter(const I8Args<V>& a, u32 group) {
+    const I8Group g = load_group(a.groups + a.first + group);
+    Cursor c;
+    c.group = __builtin_amdgcn_readfirstlane(group);
+    c.block = 0;
+    c.blocks = __builtin_amdgcn_readfirstlane((g.n_terms + 31) / 32);  // (at least one)
+    c.list = __builtin_amdgcn_readfirstlane(g.list);
+    c.table = __builtin_amdgcn_readfirstlane(g.table);
+    return c;
+}
+template <typename V>
+__device__ __forceinline__ void step(Cursor& c, const I8Args<V>& a, u32 end) {  // after the last block of the run the cursor stays
+    if (c.block + 1 < c.blocks) c.block++;
+    else if (c.group + 1 < end) c = enter(a, c.group + 1);
+}
+
+template <typename V, int ND>
+__device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb_const, u32 part, u32 row, u32 begin, u32 end, Ends* lds) {
+    const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
+    constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit of eight bytes
+    const u32 comp = row & 1, limb = row >> 1;
+    const u32 slot = part * whole_slots<V>() + (wave * 32 + lane % 32) * PER;
+    const size_t at = ((size_t)comp * a.limbs + limb) * a.N + slot;
+    const u32 ct_stride = 2 * a.limbs * a.N * sizeof(V);     // bytes
+    const char* x_base = reinterpret_cast<const char*>(a.ct_in + at);
+    const size_t out_stride = (size_t)2 * a.limbs * a.N;
+    V* const dst0 = a.out + at;
+    for (u32 i = threadIdx.x; i < (end - begin) * 32; i += THREADS) {
+        const I8Group& g = a.groups[a.first + begin + i / 32];
+        if (i % 32 < g.count) lds[i] = ends_of(a, row, g.out0 + i % 32);
+    }
+    const End<V> fin = end_of(a, c, limb_const, row, slot);
+    __syncthreads();
+
+    Cursor cur = enter(a, begin), nxt = cur;
+    step(nxt, a, end);
+    Cursor after = nxt;
+    step(after, a, end);
+    u32 idx[16];
+    u32x2 x[16];
+    v4i w, w_next;
+    auto request_idx = [&](const Cursor& p) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(a.lists + (size_t)(p.list + p.block) * 32 + half * 16 + 4 * j);
+#pragma unroll
+            for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
+        }
+    };
+    auto request_x = [&] {
+#pragma unroll
+        for (int j = 0; j < 16; j++) x[j] = *reinterpret_cast<const u32x2*>(x_base + (u64)idx[j] * ct_stride);
+    };
+    auto request_w = [&](const Cursor& p) { return a.table[(size_t)(p.table + p.block) * 64 + lane]; };
+    request_idx(cur);
+    w = request_w(cur);
+    request_x();
+    request_idx(nxt);
+    v16i sums[2 * ND];
+    while (true) {
+        const bool first = cur.block == 0, last = cur.block + 1 == cur.blocks;
+        if (first) {
+#pragma unroll
+            for (int d = 0; d < 2 * ND; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) sums[d][i] = 0;
+        }
+        v4i in[2 * ND];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            u32 lo[ND], hi[ND];
+            // the second half's bytes start at byte ND
+            auto up = [&](int k) -> u32 { return ND == 4 ? x[k][1] : __builtin_amdgcn_alignbyte(x[k][1], x[k][0], ND); };
+            transpose4<ND>(x[4 * j][0], x[4 * j + 1][0], x[4 * j + 2][0], x[4 * j + 3][0], lo);
+            transpose4<ND>(up(4 * j), up(4 * j + 1), up(4 * j + 2), up(4 * j + 3), hi);
+#pragma unroll
+            for (int d = 0; d < ND; d++) in[d][j] = (int)lo[d], in[ND + d][j] = (int)hi[d];
+        }
+        w_next = request_w(nxt);
+        request_x();
+        request_idx(after);
+#pragma unroll
+        for (int d = 0; d < 2 * ND; d++) sums[d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, in[d], sums[d], 0, 0, 0);
+        w = w_next;
+        if (last) {
+            const I8Group g = load_group(a.groups + a.first + cur.group);
+            const Ends* ends = lds + (cur.group - begin) * 32;
+            V* const dst = dst0 + g.out0 * out_stride;
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                if (8 * (u32)(r / 4) >= g.count) break;      // (rows of both halves)
+                const u32 o = 8 * (r / 4) + 4 * half + r % 4;
+                if (o < g.count) {
+                    const Ends e = ends[o];
+                    auto sum = [&](int h) {
+                        return fin.template half<ND>(sums[h * ND][r], sums[h * ND + 1][r], ND > 2 ? sums[h * ND + (ND > 2 ? 2 : 0)][r] : 0,
+                                                     ND > 3 ? sums[h * ND + (ND > 3 ? 3 : 0)][r] : 0);
+                    };
+                    V* const p = dst + o * out_stride;
+                    if constexpr (sizeof(V) == 8) {
+                        u64 v = fin.finish(fin.join(sum(0), sum(1)), e.channel, e.bias, 0);
+                        if (fin.accumulate) v = add_mod(v, *p, fin.q);
+                        *p = v;
+                    } else {
+                        u32x2 v;
+                        v[0] = (u32)fin.finish(sum(0), e.channel, e.bias, 0);
+                        v[1] = (u32)fin.finish(sum(1), e.channel, e.bias, 1);
+                        if (fin.accumulate) {
+                            const u32x2 old = *reinterpret_cast<const u32x2*>(p);
+                            v[0] = (u32)add_mod(v[0], old[0], fin.q);
+                            v[1] = (u32)add_mod(v[1], old[1], fin.q);
+                        }
+                        *reinterpret_cast<u32x2*>(p) = v;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);           // one output at a time: its temporaries are few
+            }
+            if (cur.group + 1 >= end) break;
+        }
+        cur = nxt;
+        nxt = after;
+        step(after, a, end);
+    }
+}
+
+// Workgroups go to the eight XCDs round-robin: the eight slices of a run of slots fastest, then the runs of groups, so that what reads one
+// slice runs on one XCD, close in time, and finds its inputs in that L2.
+struct Place {
+    u32 part, run, row;
+};
+__device__ __forceinline__ Place place_of(u32 parts, u32 runs) {
+    const u32 side = min(parts, 8u);  // (parts is a power of two, below eight for packed residues at N = 2^10)
+    u32 b = blockIdx.x / side;
+    const u32 run = b % runs;
+    b /= runs;
+    return Place{b % (parts / side) * side + blockIdx.x % side, run, b / (parts / side)};
+}
+
+template <typename V>
+__global__ void __launch_bounds__(THREADS, 2) i8_whole_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
+    __shared__ Ends lds[WHOLE_RUN * 32];
+    const Place at = place_of(a.N / whole_slots<V>(), a.runs);
+    const u32 begin = at.run * a.run, end = min(begin + a.run, a.n_groups);
+    const LimbConst& c = lt.c[at.row >> 1];
+    const I8Limb& l = lc.c[at.row >> 1];
+    if constexpr (sizeof(V) == 4) whole_body<V, 4>(a, c, l, at.part, at.row, begin, end, lds);
+    else if (l.nd == 4) whole_body<V, 4>(a, c, l, at.part, at.row, begin, end, lds);
+    else if (l.nd == 3) whole_body<V, 3>(a, c, l, at.part, at.row, begin, end, lds);
+    else whole_body<V, 2>(a, c, l, at.part, at.row, begin, end, lds);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Second form: OT tiles of 32 outputs.
+
 template <typename V, int OT, int ND>
-__device__ __forceinline__ void i8_body(const I8Args<V>& a, const LimbConst& c, const I8Group& g, u32 part, u32 row, u64* exchange) {
+__device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb_const, const I8Group& g, u32 part, u32 row, Ends* ends,
+                                           u64* exchange) {
     const u32 lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const u32 comp = row & 1, limb = row >> 1;
     const u32 upper = sizeof(V) == 8 ? wave & 1 : 0;         // which half of the digits
-    const u32 slot = part * Form<V>::SLOTS + wave / Form<V>::PARTS * 32 + lane % 32;
+    const u32 slot = part * split_slots<V>() + (sizeof(V) == 8 ? wave / 2 : wave) * 32 + lane % 32;
     const size_t at = ((size_t)comp * a.limbs + limb) * a.N + slot;
     const u32 ct_stride = 2 * a.limbs * a.N * sizeof(V);     // bytes
     const char* x_base = reinterpret_cast<const char*>(a.ct_in + at) + upper * ND;
     const u32 blocks = (g.n_terms + 31) / 32;
+    const u32* list = a.lists + (size_t)g.list * 32 + half * 16;
+    const v4i* table = a.table + (size_t)g.table * 64 + lane;
+    if (threadIdx.x < g.count) ends[threadIdx.x] = ends_of(a, row, g.out0 + threadIdx.x);
 
     v16i sums[OT][ND];
 #pragma unroll
@@ -105,71 +356,93 @@ __device__ __forceinline__ void i8_body(const I8Args<V>& a, const LimbConst& c, 
 #pragma unroll
             for (int i = 0; i < 16; i++) sums[o][d][i] = 0;
 
-    const u32* list = a.lists + (size_t)g.list * 32 + half * 16;
-    const v4i* table = a.table + (size_t)g.table * 64 + lane;
-    for (u32 b = 0; b < blocks; b++) {
-        u32 x[16];
+    // Block b is multiplied while the inputs of blocks b + 1 and b + 2 are on their way and the list of block b + 3 is; past the end the last block's
+    // are requested again.
+    u32 idx[16], x[2][16];
+    v4i w[OT];
+    auto request_idx = [&](u32 b) {
+        const u32* p = list + (size_t)min(b, blocks - 1) * 32;
 #pragma unroll
-        for (int j = 0; j < 16; j++) x[j] = *reinterpret_cast<const u32_any*>(x_base + (u64)list[b * 32 + j] * ct_stride);
+        for (int j = 0; j < 4; j++) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * j);
+#pragma unroll
+            for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
+        }
+    };
+    auto request_x = [&](u32 (&to)[16]) {
+#pragma unroll
+        for (int j = 0; j < 16; j++) to[j] = *reinterpret_cast<const u32_any*>(x_base + (u64)idx[j] * ct_stride);
+    };
+    auto request_w = [&](u32 b) {
+#pragma unroll
+        for (int o = 0; o < OT; o++) w[o] = table[((size_t)min(b, blocks - 1) * OT + o) * 64];
+    };
+    auto multiply = [&](u32 (&from)[16], u32 b) {
         v4i in[ND];
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             u32 t[ND];
-            transpose4<ND>(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3], t);
+            transpose4<ND>(from[4 * j], from[4 * j + 1], from[4 * j + 2], from[4 * j + 3], t);
 #pragma unroll
             for (int d = 0; d < ND; d++) in[d][j] = (int)t[d];
         }
+        v4i now[OT];
 #pragma unroll
-        for (int o = 0; o < OT; o++) {
-            const v4i w = table[(b * OT + o) * 64];
+        for (int o = 0; o < OT; o++) now[o] = w[o];
+        request_w(b + 1);
+        request_x(from);
+        request_idx(b + 3);
 #pragma unroll
-            for (int d = 0; d < ND; d++) sums[o][d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, in[d], sums[o][d], 0, 0, 0);
+        for (int o = 0; o < OT; o++)
+#pragma unroll
+            for (int d = 0; d < ND; d++) sums[o][d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now[o], in[d], sums[o][d], 0, 0, 0);
+    };
+    if (blocks) {
+        request_idx(0);
+        request_w(0);
+        request_x(x[0]);
+        request_idx(1);
+        request_x(x[1]);
+        request_idx(2);
+        u32 b = 0;
+        for (; b + 1 < blocks; b += 2) {
+            multiply(x[0], b);
+            multiply(x[1], b + 1);
         }
+        if (b < blocks) multiply(x[0], b);
     }
 
-    // the ends of the outputs: tiles of 32, of which a lane holds 16 at its slot
-    u64 tok = 0, tok_shoup = 0;
-    if (a.token) {
-        tok = a.token[(size_t)limb * a.N + slot];
-        tok_shoup = shoup_companion(tok, c);
-    }
+    const End<V> fin = end_of(a, c, limb_const, row, slot);
     const size_t out_stride = (size_t)2 * a.limbs * a.N;
-    auto store = [&](u32 o, u64 v) {  // v < 4q, congruent to the scaled sum without the addend
-        v = v >= c.two_q ? v - c.two_q : v;
-        v += a.addend[(size_t)limb * a.n_out + g.out0 + o];
-        v = v >= c.two_q ? v - c.two_q : v;
-        v = v >= c.q ? v - c.q : v;
-        if (a.token) v = shoup_mul(v, tok, tok_shoup, c.q);
-        if (a.bias && comp == 0) v = add_mod(v, a.bias[(size_t)(g.out0 + o) * a.limbs + limb], c.q);
-        V* dst = a.out + (g.out0 + o) * out_stride + at;
-        if (a.accumulate) v = add_mod(v, *dst, c.q);
-        *dst = (V)v;
-    };
-    // this lane's output r (0 .. 15) of tile o, and its part of the sum, below 2q
+    V* const dst = a.out + g.out0 * out_stride + at;
     auto output_of = [&](int o, int r) -> u32 { return 32 * o + 8 * (r / 4) + 4 * half + r % 4; };
-    auto part_of = [&](int o, int r) -> u64 {
-        const u32 mine = min(output_of(o, r), g.count - 1);
-        const I8Mult m = a.mult[((size_t)limb * a.n_out + g.out0 + mine) * 2 + upper];
-        int64_t y = 1ll << OFFSET_BITS;
-#pragma unroll
-        for (int d = 0; d < ND; d++) y += (int64_t)sums[o][d][r] << (8 * d);
-        return shoup_mul_lazy((u64)y, m.w, m.w_shoup, c.q);
+    auto sum = [&](int o, int r) {
+        return fin.template half<ND>(sums[o][0][r], sums[o][1][r], ND > 2 ? sums[o][ND > 2 ? 2 : 0][r] : 0, ND > 3 ? sums[o][ND > 3 ? 3 : 0][r] : 0);
+    };
+    auto store = [&](u32 o, u64 r) {
+        if (o >= g.count) return;
+        const Ends e = ends[o];
+        u64 v = fin.finish(r, e.channel, e.bias, 0);
+        V* const p = dst + o * out_stride;
+        if (fin.accumulate) v = add_mod(v, *p, fin.q);
+        *p = (V)v;
     };
     if constexpr (sizeof(V) == 8) {
         // of every tile the wavefront of the lower digits finishes the first eight of a lane's outputs, the other one the last eight
         auto finish = [&](auto of_upper) {
-            constexpr int KEEP = decltype(of_upper)::value ? 8 : 0, SEND = 8 - KEEP;
+            constexpr bool UPPER = decltype(of_upper)::value;
+            constexpr int KEEP = UPPER ? 8 : 0, SEND = 8 - KEEP;
 #pragma unroll
             for (int o = 0; o < OT; o++) {
                 if (32 * (u32)o >= g.count) break;
                 u64* buf = exchange + (o & 1) * (WAVES * 8 * 64) + lane;
 #pragma unroll
-                for (int k = 0; k < 8; k++) buf[(wave * 8 + k) * 64] = part_of(o, SEND + k);
-                lds_barrier();
+                for (int k = 0; k < 8; k++) buf[(wave * 8 + k) * 64] = sum(o, SEND + k);
+                lds_barrier();  // (also for the ends)
 #pragma unroll
                 for (int k = 0; k < 8; k++) {
-                    const u64 v = part_of(o, KEEP + k) + buf[((wave ^ 1) * 8 + k) * 64];
-                    if (output_of(o, KEEP + k) < g.count) store(output_of(o, KEEP + k), v);
+                    const u64 mine = sum(o, KEEP + k), other = buf[((wave ^ 1) * 8 + k) * 64];
+                    store(output_of(o, KEEP + k), UPPER ? fin.join(other, mine) : fin.join(mine, other));
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -177,13 +450,13 @@ __device__ __forceinline__ void i8_body(const I8Args<V>& a, const LimbConst& c, 
         if (upper) finish(std::true_type{});
         else finish(std::false_type{});
     } else {
+        lds_barrier();
 #pragma unroll
         for (int o = 0; o < OT; o++) {
             if (32 * (u32)o >= g.count) break;
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const u64 v = part_of(o, r);
-                if (output_of(o, r) < g.count) store(output_of(o, r), v);
+                store(output_of(o, r), sum(o, r));
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -191,44 +464,48 @@ __device__ __forceinline__ void i8_body(const I8Args<V>& a, const LimbConst& c, 
 }
 
 template <typename V, int OT>
-__global__ void __launch_bounds__(THREADS, OT == 1 ? 3 : OT == 2 ? 2 : 1) i8_mac_kernel(LimbTable lt, I8Nd nd, I8Args<V> a) {
+__global__ void __launch_bounds__(THREADS, OT == 2 ? 2 : 1) i8_split_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
+    __shared__ Ends ends[32 * OT];
     __shared__ u64 exchange[sizeof(V) == 8 ? 2 * WAVES * 8 * 64 : 1];
-    // Workgroups go to the eight XCDs round-robin: the eight slices of a run of slots fastest, then the groups, so that the groups
-    // that read one slice run on one XCD, close in time, and find its inputs in that L2.
-    const u32 parts8 = a.N / Form<V>::SLOTS / 8;
-    u32 b = blockIdx.x / 8;
-    const u32 group = b % a.n_groups;
-    b /= a.n_groups;
-    const u32 part = b % parts8 * 8 + blockIdx.x % 8, row = b / parts8;
-    const I8Group g = a.groups[a.first + group];
-    const LimbConst& c = lt.c[row >> 1];
-    const u32 digits = sizeof(V) == 8 ? nd.nd[row >> 1] : 4;
-    if (digits == 4) i8_body<V, OT, 4>(a, c, g, part, row, exchange);
-    else if constexpr (sizeof(V) == 8) {
-        if (digits == 3) i8_body<V, OT, 3>(a, c, g, part, row, exchange);
-        else i8_body<V, OT, 2>(a, c, g, part, row, exchange);
-    }
+    const Place at = place_of(a.N / split_slots<V>(), a.runs);
+    const I8Group g = load_group(a.groups + a.first + at.run);
+    const LimbConst& c = lt.c[at.row >> 1];
+    const I8Limb& l = lc.c[at.row >> 1];
+    if constexpr (sizeof(V) == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, exchange);
+    else if (l.nd == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, exchange);
+    else if (l.nd == 3) split_body<V, OT, 3>(a, c, l, g, at.part, at.row, ends, exchange);
+    else split_body<V, OT, 2>(a, c, l, g, at.part, at.row, ends, exchange);
 }
 
 template <typename V>
-u64 class_blocks(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls) {
-    return (u64)(l->class_begin[cls + 1] - l->class_begin[cls]) * (ctx->N / Form<V>::SLOTS) * 2 * limbs;
+u32 class_count(const he_i8_layer* l, u32 cls) { return l->class_begin[cls + 1] - l->class_begin[cls]; }
+
+// workgroups of a class; *run: the groups that each of them takes
+template <typename V>
+u64 class_blocks(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls, u32* run) {
+    const u64 rows = 2 * limbs, parts = ctx->N / (cls == 0 ? whole_slots<V>() : split_slots<V>()), count = class_count<V>(l, cls);
+    *run = cls == 0 ? WHOLE_RUN : 1;
+    while (*run > 1 && (count + *run - 1) / *run * parts * rows < MIN_WORKGROUPS) *run /= 2;
+    return (count + *run - 1) / *run * parts * rows;
 }
 
 template <typename V, int OT>
 int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) {
     a.first = l->class_begin[OT - 1];
-    a.n_groups = l->class_begin[OT] - a.first;
+    a.n_groups = class_count<V>(l, OT - 1);
     if (a.n_groups == 0) return HE_OK;
-    hipLaunchKernelGGL((i8_mac_kernel<V, OT>), dim3((u32)class_blocks<V>(ctx, l, a.limbs, OT - 1)), dim3(THREADS), 0, s, ctx->limbs, l->nd, a);
+    const dim3 grid((u32)class_blocks<V>(ctx, l, a.limbs, OT - 1, &a.run)), block(THREADS);
+    a.runs = (a.n_groups + a.run - 1) / a.run;
+    if constexpr (OT == 1) hipLaunchKernelGGL(i8_whole_kernel<V>, grid, block, 0, s, ctx->limbs, l->limbs, a);
+    else hipLaunchKernelGGL((i8_split_kernel<V, OT>), grid, block, 0, s, ctx->limbs, l->limbs, a);
     HE_HIP(hipGetLastError());
     return HE_OK;
 }
 
 template <typename V>
 int launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const V* ct_in, const V* token, const u64* bias, V* out, u32 accumulate, hipStream_t s) {
-    const I8Args<V> a{l->groups_dev, l->lists_dev, reinterpret_cast<const v4i*>(l->table_dev), l->mult_dev, sizeof(V) == 8 ? l->addend_dev : l->addend32_dev,
-                      ct_in, token, bias, out, limbs, ctx->N, l->n_out, 0, 0, accumulate};
+    const I8Args<V> a{l->groups_dev, l->lists_dev, reinterpret_cast<const v4i*>(l->table_dev), sizeof(V) == 8 ? l->channels_dev : l->channels32_dev,
+                      ct_in, token, bias, out, limbs, ctx->N, l->n_out, 0, 0, 0, 0, accumulate};
     int rc;
     if ((rc = launch_class<V, 1>(ctx, a, l, s)) != HE_OK) return rc;
     if ((rc = launch_class<V, 2>(ctx, a, l, s)) != HE_OK) return rc;
@@ -251,8 +528,9 @@ struct Rows {
 
 // every launch of a call must fit a grid
 int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed) {
+    u32 run;
     for (u32 cls = 0; cls < I8_CLASSES; cls++)
-        if ((packed ? class_blocks<u32>(ctx, l, limbs, cls) : class_blocks<u64>(ctx, l, limbs, cls)) > 0x7FFFFFFFull) return HE_ERR_RANGE;
+        if ((packed ? class_blocks<u32>(ctx, l, limbs, cls, &run) : class_blocks<u64>(ctx, l, limbs, cls, &run)) > 0x7FFFFFFFull) return HE_ERR_RANGE;
     return HE_OK;
 }
 
@@ -267,8 +545,9 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
     for (u32 o = 0; o < n_out;) {
         u32 end = o + 1;
         while (end < n_out && rows.same_inputs(o, end)) end++;
-        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + I8_CLASSES - 1) / I8_CLASSES, per = (tiles + cuts - 1) / cuts;
         const u32 terms = rows.terms(o), blocks = (terms + 31) / 32;
+        // (outputs without terms go to the second form, whose loop over the blocks may be empty)
+        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + I8_CLASSES - 1) / I8_CLASSES, per = std::max((tiles + cuts - 1) / cuts, terms ? 1u : 2u);
         const u32 list = (u32)(h.lists.size() / 32);
         for (u32 t = 0; t < blocks * 32; t++) h.lists.push_back(term_ct[off[o] + std::min(t, terms - 1)]);
         for (; o < end; o += std::min(per * 32, end - o)) {
@@ -302,33 +581,28 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
         h.groups.insert(h.groups.end(), classes[cls].begin(), classes[cls].end());
     }
     l->class_begin[I8_CLASSES] = (u32)h.groups.size();
-    // Per limb and output: the multipliers of the two halves of a sum and the constant that goes with them.
+    // Per limb and output: the scale and the constant that goes with it.
     std::vector<int64_t> weight_sum(n_out);
     for (u32 o = 0; o < n_out; o++)
         for (u32 t = off[o]; t < off[o + 1]; t++) weight_sum[o] += weights[term_pt[t]];
-    h.mult.resize((size_t)ctx->L * n_out * 2);
-    h.addend.resize((size_t)ctx->L * n_out);
-    h.addend32.resize((size_t)ctx->L * n_out);
+    h.channels.resize((size_t)ctx->L * n_out);
+    h.channels32.resize((size_t)ctx->L * n_out);
     for (u32 i = 0; i < ctx->L; i++) {
         const u64 q = ctx->q[i];
         u32 bits = 0;
         while (q >> bits) bits++;
         const u32 nd = std::max<u32>(2, ((bits + 7) / 8 + 1) / 2);
-        l->nd.nd[i] = nd;
         const u64 shift = (u64)(((u128)1 << (8 * nd)) % q), offset = (1ull << OFFSET_BITS) % q;
-        u64 flipped = 0, flipped32 = 0;  // what the digits' top bits stand for, all 2 nd of them, and four
+        l->limbs.c[i] = I8Limb{nd, q < (1ull << 61), shift, (u64)(((u128)shift << 64) / q)};
+        u64 flipped = 0;  // what the digits' top bits stand for, all 2 nd of them
         for (u32 d = 0; d < 2 * nd; d++) flipped |= 0x80ull << (8 * d);
-        flipped32 = 0x80808080u % q;
-        flipped %= q;
+        const u64 both = (u64)(((u128)offset + mul_mod_host(offset, shift, q)) % q);
         for (u32 o = 0; o < n_out; o++) {
-            const size_t k = (size_t)i * n_out + o;
-            const u64 s = scale ? scale[(size_t)o * ctx->L + i] : 1 % q, t = mul_mod_host(s, shift, q);
-            h.mult[2 * k] = I8Mult{s, (u64)(((u128)s << 64) / q)};
-            h.mult[2 * k + 1] = I8Mult{t, (u64)(((u128)t << 64) / q)};
+            const u64 s = scale ? scale[(size_t)o * ctx->L + i] : 1, s_shoup = (u64)(((u128)s << 64) / q);
             const u64 sum = (u64)(((__int128)weight_sum[o] % (__int128)q + q) % q);
-            const u64 both = (u64)(((u128)offset + mul_mod_host(offset, shift, q)) % q);
-            h.addend[k] = mul_mod_host(s, (mul_mod_host(flipped, sum, q) + q - both) % q, q);
-            h.addend32[k] = mul_mod_host(s, (mul_mod_host(flipped32, sum, q) + q - offset) % q, q);
+            const size_t k = (size_t)i * n_out + o;
+            h.channels[k] = I8Channel{s, s_shoup, mul_mod_host(s, (mul_mod_host(flipped % q, sum, q) + q - both) % q, q)};
+            h.channels32[k] = I8Channel{s, s_shoup, mul_mod_host(s, (mul_mod_host(0x80808080u % q, sum, q) + q - offset) % q, q)};
         }
     }
 }

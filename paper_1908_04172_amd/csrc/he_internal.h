@@ -161,34 +161,37 @@ struct I8Group {
     u32 table;     // where the weights start in he_i8_layer::table_dev, in tiles of 1024 bytes
     u32 pad[3];
 };
-// What one half of an output's sum is multiplied by: a residue and its Shoup companion.
-struct I8Mult {
-    u64 w, w_shoup;
+// An output's scale modulo a limb, its Shoup companion, and what is left to add (he_i8.hip).
+struct I8Channel {
+    u64 s, s_shoup, addend;
 };
-// Per limb: the digits of a residue that each of two wavefronts takes (2, 3 or 4).
-struct I8Nd {
-    u32 nd[HE_MAX_LIMBS];
+// Per limb: how many digits of a residue one half of them has (2, 3 or 4), and 256^nd mod q with its Shoup companion.
+struct I8Limb {
+    u32 nd;
+    u32 cheap;  // 1: q < 2^61, the cheap quotient estimate serves
+    u64 shift, shift_shoup;
+};
+struct I8Limbs {
+    I8Limb c[HE_MAX_LIMBS];
 };
 struct he_i8_layer {
     he_ctx* ctx;
     int device;
     u32 n_in, n_out, n_terms;
     u32 class_begin[I8_CLASSES + 1];  // groups sorted by the tiles of 32 outputs that they take
-    I8Nd nd;
+    I8Limbs limbs;
     I8Group* groups_dev;
     u32* lists_dev;    // the groups' ciphertexts, padded to blocks of 32 with the last one
     int8_t* table_dev; // the weights as the matrix instructions take them, shared by groups with the same ones
-    I8Mult* mult_dev;  // [L][n_out][2]
-    u64* addend_dev;   // [L][n_out]: what the offsets of a sum leave to add, times the channel's scale
-    u64* addend32_dev; // ... in packed storage
+    I8Channel* channels_dev;    // [L][n_out]
+    I8Channel* channels32_dev;  // ... for packed storage
 };
 // What of a layer is built on the host.
 struct I8Host {
     std::vector<I8Group> groups;
     std::vector<u32> lists;
     std::vector<int8_t> table;
-    std::vector<I8Mult> mult;
-    std::vector<u64> addend, addend32;
+    std::vector<I8Channel> channels, channels32;
 };
 
 #define HE_HIP(call)                                   \
