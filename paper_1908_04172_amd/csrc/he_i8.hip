@@ -31,7 +31,6 @@ namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
-typedef u32 u32_any __attribute__((aligned(1)));                            // four bytes of a residue, at any byte
 typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 constexpr u32 THREADS = 256, WAVES = THREADS / 64;
@@ -39,11 +38,11 @@ constexpr int OFFSET_BITS = 56;      // what makes a half of a sum positive
 constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most
 constexpr u64 MIN_WORKGROUPS = 2048; // ... while the launch keeps at least this many workgroups
 
-// slots of a workgroup: first form (32 units of eight bytes per wavefront), second form (two wavefronts per slot, or one)
+// slots of a workgroup: 32 units of eight bytes per wavefront in the first form, 64 in all in the second
 template <typename V>
 __host__ __device__ constexpr u32 whole_slots() { return 32 * WAVES * 8 / sizeof(V); }
 template <typename V>
-__host__ __device__ constexpr u32 split_slots() { return 32 * WAVES * 4 / sizeof(V); }
+__host__ __device__ constexpr u32 split_slots() { return 64 * 8 / sizeof(V); }
 
 template <typename V>
 struct I8Args {
@@ -101,13 +100,25 @@ __device__ __forceinline__ u64 shoup_companion(u64 w, const LimbConst& c) {
     return e;
 }
 
-// What the ends of all outputs of a row have in common.
+// What the end of an output reads from the LDS.  Without tokens the bias is part of the addend.
+struct Ends {
+    u64 s, s_shoup, addend, bias;
+};
 template <typename V>
+__device__ __forceinline__ Ends ends_of(const I8Args<V>& a, const LimbConst& c, u32 row, u32 output) {
+    const I8Channel ch = a.channels[(size_t)(row >> 1) * a.n_out + output];
+    const u64 bias = a.bias && !(row & 1) ? a.bias[(size_t)output * a.limbs + (row >> 1)] : 0;
+    return Ends{ch.s, ch.s_shoup, a.token ? ch.addend : add_mod(ch.addend, bias, c.q), bias};
+}
+
+// What the ends of all outputs of a row have in common.
+template <typename V, int UNITS>
 struct End {
+    static constexpr int SLOTS = UNITS * 8 / sizeof(V);
     u64 q, two_q;
     I8Limb limb;
-    u64 tok[sizeof(V) == 8 ? 1 : 2], tok_shoup[sizeof(V) == 8 ? 1 : 2];  // the tokens of this lane's slots
-    bool has_token, has_bias, accumulate;
+    u64 tok[SLOTS], tok_shoup[SLOTS];  // the tokens of this lane's slots
+    bool has_token, accumulate;
     int32_t b8, b16, b24;     // 2^8, 2^16, 2^24 as data (multiplied by a literal they become shifts and additions)
 
     // the sum of one half's digits, made positive
@@ -119,39 +130,51 @@ struct End {
         if constexpr (ND > 3) v = (int64_t)s3 * b24 + v;
         return (u64)v;
     }
-    // both halves -> what the channel's scale multiplies: any 64-bit value congruent to the sum
+    // both halves -> what the channel's scale multiplies: a 64-bit value congruent to the sum, below 4q + 2^57 for q < 2^61, else 2q + 2^57
     __device__ __forceinline__ u64 join(u64 y0, u64 y1) const {
-        const u64 up = limb.cheap ? shoup_mul_lazy4(y1, limb.shift, limb.shift_shoup, q) : shoup_mul_lazy(y1, limb.shift, limb.shift_shoup, q);
-        return y0 + up;  // below 4q + 2^57 for q < 2^61, else below 2q + 2^57
+        return shoup_remainder_add(y1, limb.shift, limb.cheap ? shoup_quotient_cheap(y1, limb.shift_shoup) : shoup_quotient(y1, limb.shift_shoup), q, y0);
     }
     // the residue of an output
-    __device__ __forceinline__ u64 finish(u64 r, const I8Channel& ch, u64 bias, int k) const {
-        u64 v = shoup_mul_lazy(r, ch.s, ch.s_shoup, q) + ch.addend;  // below 3q
+    __device__ __forceinline__ u64 finish(u64 r, const Ends& e, int k) const {
+        u64 v = shoup_remainder_add(r, e.s, shoup_quotient(r, e.s_shoup), q, e.addend);  // below 3q
         if (has_token) {
-            v = v >= two_q ? v - two_q : v;
-            v = shoup_mul_lazy(v, tok[k], tok_shoup[k], q);
+            v = shoup_remainder_add(v, tok[k], shoup_quotient(v, tok_shoup[k]), q, e.bias);
         }
-        v += bias;                                                   // below 4q
         v = v >= two_q ? v - two_q : v;
         return v >= q ? v - q : v;
     }
+    // an output at UNITS neighbouring units, from the sums of their halves
+    __device__ __forceinline__ void store(V* p, const Ends& e, const u64 (&y0)[UNITS], const u64 (&y1)[UNITS]) const {
+        typedef V piece __attribute__((ext_vector_type(SLOTS), aligned(8)));
+        piece v;
+#pragma unroll
+        for (int k = 0; k < UNITS; k++) {
+            if constexpr (sizeof(V) == 8) v[k] = finish(join(y0[k], y1[k]), e, k);
+            else v[2 * k] = (V)finish(y0[k], e, 2 * k), v[2 * k + 1] = (V)finish(y1[k], e, 2 * k + 1);
+        }
+        if (accumulate) {
+            const piece old = *reinterpret_cast<const piece*>(p);
+#pragma unroll
+            for (int k = 0; k < SLOTS; k++) v[k] = (V)add_mod(v[k], old[k], q);
+        }
+        *reinterpret_cast<piece*>(p) = v;
+    }
 };
 
-template <typename V>
-__device__ __forceinline__ End<V> end_of(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb, u32 row, u32 slot) {
-    End<V> e;
+template <typename V, int UNITS>
+__device__ __forceinline__ End<V, UNITS> end_of(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb, u32 row, u32 slot) {
+    End<V, UNITS> e;
     e.q = c.q;
     e.two_q = c.two_q;
     e.limb = limb;
     e.has_token = a.token != nullptr;
-    e.has_bias = a.bias != nullptr && !(row & 1);
     e.accumulate = a.accumulate;
     e.b8 = 1 << 8;
     e.b16 = 1 << 16;
     e.b24 = 1 << 24;
     asm volatile("" : "+s"(e.b8), "+s"(e.b16), "+s"(e.b24));
 #pragma unroll
-    for (u32 k = 0; k < sizeof(e.tok) / sizeof(u64); k++) {
+    for (int k = 0; k < e.SLOTS; k++) {
         e.tok[k] = e.tok_shoup[k] = 0;
         if (e.has_token) {
             e.tok[k] = a.token[(size_t)(row >> 1) * a.N + slot + k];
@@ -159,16 +182,6 @@ __device__ __forceinline__ End<V> end_of(const I8Args<V>& a, const LimbConst& c,
         }
     }
     return e;
-}
-
-// An output's channel and bias, which the ends read from the LDS.
-struct Ends {
-    I8Channel channel;
-    u64 bias;
-};
-template <typename V>
-__device__ __forceinline__ Ends ends_of(const I8Args<V>& a, u32 row, u32 output) {
-    return Ends{a.channels[(size_t)(row >> 1) * a.n_out + output], a.bias && !(row & 1) ? a.bias[(size_t)output * a.limbs + (row >> 1)] : 0};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -208,9 +221,9 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
     V* const dst0 = a.out + at;
     for (u32 i = threadIdx.x; i < (end - begin) * 32; i += THREADS) {
         const I8Group& g = a.groups[a.first + begin + i / 32];
-        if (i % 32 < g.count) lds[i] = ends_of(a, row, g.out0 + i % 32);
+        if (i % 32 < g.count) lds[i] = ends_of(a, c, row, g.out0 + i % 32);
     }
-    const End<V> fin = end_of(a, c, limb_const, row, slot);
+    const End<V, 1> fin = end_of<V, 1>(a, c, limb_const, row, slot);
     __syncthreads();
 
     Cursor cur = enter(a, begin), nxt = cur;
@@ -220,23 +233,23 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
     u32 idx[16];
     u32x2 x[16];
     v4i w, w_next;
-    auto request_idx = [&](const Cursor& p) {
+    auto request_idx = [&](const Cursor& p, int j) {  // four terms
+        const u32x4 v = *reinterpret_cast<const u32x4*>(a.lists + (size_t)(p.list + p.block) * 32 + half * 16 + 4 * j);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(a.lists + (size_t)(p.list + p.block) * 32 + half * 16 + 4 * j);
-#pragma unroll
-            for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
-        }
+        for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
     };
-    auto request_x = [&] {
+    auto request_x = [&](int j) {
 #pragma unroll
-        for (int j = 0; j < 16; j++) x[j] = *reinterpret_cast<const u32x2*>(x_base + (u64)idx[j] * ct_stride);
+        for (int k = 4 * j; k < 4 * j + 4; k++) x[k] = *reinterpret_cast<const u32x2*>(x_base + (u64)idx[k] * ct_stride);
     };
     auto request_w = [&](const Cursor& p) { return a.table[(size_t)(p.table + p.block) * 64 + lane]; };
-    request_idx(cur);
     w = request_w(cur);
-    request_x();
-    request_idx(nxt);
+#pragma unroll
+    for (int j = 0; j < 4; j++) request_idx(cur, j);
+#pragma unroll
+    for (int j = 0; j < 4; j++) request_x(j);
+#pragma unroll
+    for (int j = 0; j < 4; j++) request_idx(nxt, j);
     v16i sums[2 * ND];
     while (true) {
         const bool first = cur.block == 0, last = cur.block + 1 == cur.blocks;
@@ -247,8 +260,9 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
                 for (int i = 0; i < 16; i++) sums[d][i] = 0;
         }
         v4i in[2 * ND];
+        w_next = request_w(nxt);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < 4; j++) {  // (four terms at a time, whose registers take those of the next block)
             u32 lo[ND], hi[ND];
             // the second half's bytes start at byte ND
             auto up = [&](int k) -> u32 { return ND == 4 ? x[k][1] : __builtin_amdgcn_alignbyte(x[k][1], x[k][0], ND); };
@@ -256,10 +270,10 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
             transpose4<ND>(up(4 * j), up(4 * j + 1), up(4 * j + 2), up(4 * j + 3), hi);
 #pragma unroll
             for (int d = 0; d < ND; d++) in[d][j] = (int)lo[d], in[ND + d][j] = (int)hi[d];
+            request_x(j);
+            request_idx(after, j);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        w_next = request_w(nxt);
-        request_x();
-        request_idx(after);
 #pragma unroll
         for (int d = 0; d < 2 * ND; d++) sums[d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, in[d], sums[d], 0, 0, 0);
         w = w_next;
@@ -277,22 +291,8 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
                         return fin.template half<ND>(sums[h * ND][r], sums[h * ND + 1][r], ND > 2 ? sums[h * ND + (ND > 2 ? 2 : 0)][r] : 0,
                                                      ND > 3 ? sums[h * ND + (ND > 3 ? 3 : 0)][r] : 0);
                     };
-                    V* const p = dst + o * out_stride;
-                    if constexpr (sizeof(V) == 8) {
-                        u64 v = fin.finish(fin.join(sum(0), sum(1)), e.channel, e.bias, 0);
-                        if (fin.accumulate) v = add_mod(v, *p, fin.q);
-                        *p = v;
-                    } else {
-                        u32x2 v;
-                        v[0] = (u32)fin.finish(sum(0), e.channel, e.bias, 0);
-                        v[1] = (u32)fin.finish(sum(1), e.channel, e.bias, 1);
-                        if (fin.accumulate) {
-                            const u32x2 old = *reinterpret_cast<const u32x2*>(p);
-                            v[0] = (u32)add_mod(v[0], old[0], fin.q);
-                            v[1] = (u32)add_mod(v[1], old[1], fin.q);
-                        }
-                        *reinterpret_cast<u32x2*>(p) = v;
-                    }
+                    const u64 y0[1] = {sum(0)}, y1[1] = {sum(1)};
+                    fin.store(dst + o * out_stride, e, y0, y1);
                 }
                 __builtin_amdgcn_sched_barrier(0);           // one output at a time: its temporaries are few
             }
@@ -331,150 +331,178 @@ __global__ void __launch_bounds__(THREADS, 2) i8_whole_kernel(LimbTable lt, I8Li
 }
 
 // ---------------------------------------------------------------------------------------------
-// Second form: OT tiles of 32 outputs.
+// Second form: 2 OT tiles of 32 outputs.  A workgroup takes 64 units of eight bytes and 64 terms at a time: each wavefront loads 16 of the
+// terms, 16 bytes of a row per lane, transposes them and writes the operands to the LDS; then it multiplies the digits of its half by
+// its OT tiles.  Unit 2 l + k of the 64 is column l of column tile k, so that a lane ends up with two neighbouring units.
+
+// Operands of 64 terms: [block of 32 terms][digit][column tile][lane], twice (one is filled while the other is multiplied).
+constexpr u32 OPERAND_PIECES = 2 * 8 * 2 * 64;
 
 template <typename V, int OT, int ND>
 __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb_const, const I8Group& g, u32 part, u32 row, Ends* ends,
-                                           u64* exchange) {
-    const u32 lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+                                           v4i* lds) {
+    const u32 lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32, col = lane % 32;
+    constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit
     const u32 comp = row & 1, limb = row >> 1;
-    const u32 upper = sizeof(V) == 8 ? wave & 1 : 0;         // which half of the digits
-    const u32 slot = part * split_slots<V>() + (sizeof(V) == 8 ? wave / 2 : wave) * 32 + lane % 32;
+    const u32 slot = part * split_slots<V>() + col * 2 * PER;  // this lane's first, of four or two
     const size_t at = ((size_t)comp * a.limbs + limb) * a.N + slot;
     const u32 ct_stride = 2 * a.limbs * a.N * sizeof(V);     // bytes
-    const char* x_base = reinterpret_cast<const char*>(a.ct_in + at) + upper * ND;
+    const char* x_base = reinterpret_cast<const char*>(a.ct_in + at);
     const u32 blocks = (g.n_terms + 31) / 32;
-    const u32* list = a.lists + (size_t)g.list * 32 + half * 16;
-    const v4i* table = a.table + (size_t)g.table * 64 + lane;
-    if (threadIdx.x < g.count) ends[threadIdx.x] = ends_of(a, row, g.out0 + threadIdx.x);
+    const u32 upper = wave & 1, tile0 = wave / 2 * OT;       // what this wavefront multiplies
+    const u32 load_block = wave / 2, load_half = wave & 1;   // what it loads: 16 terms of one of the two blocks, eight per lane
+    const u32* list = a.lists + (size_t)g.list * 32 + load_half * 16 + half * 8;
+    const v4i* table = a.table + ((size_t)g.table + tile0) * 64 + lane;
+    if (threadIdx.x < g.count) ends[threadIdx.x] = ends_of(a, c, row, g.out0 + threadIdx.x);
 
-    v16i sums[OT][ND];
+    v16i sums[OT][2][ND];
 #pragma unroll
     for (int o = 0; o < OT; o++)
 #pragma unroll
-        for (int d = 0; d < ND; d++)
+        for (int k = 0; k < 2; k++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) sums[o][d][i] = 0;
+            for (int d = 0; d < ND; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) sums[o][k][d][i] = 0;
 
-    // Block b is multiplied while the inputs of blocks b + 1 and b + 2 are on their way and the list of block b + 3 is; past the end the last block's
-    // are requested again.
-    u32 idx[16], x[2][16];
-    v4i w[OT];
-    auto request_idx = [&](u32 b) {
-        const u32* p = list + (size_t)min(b, blocks - 1) * 32;
+    // Step s multiplies blocks 2 s and 2 s + 1 while the residues of step s + 1 become its operands; those of AHEAD steps more are
+    // on their way (one where two workgroups share a compute unit); past the end the last block's are requested again.
+    constexpr int AHEAD = OT == 1 ? 1 : 2;
+    u32 idx[8];
+    u32x4 x[AHEAD][8];
+    v4i w[2][OT];
+    auto request_idx = [&](u32 s) {
+        const u32* p = list + (size_t)min(2 * s + load_block, blocks - 1) * 32;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < 2; j++) {
             const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * j);
 #pragma unroll
             for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
         }
     };
-    auto request_x = [&](u32 (&to)[16]) {
+    auto request_x = [&](u32x4 (&to)[8]) {
 #pragma unroll
-        for (int j = 0; j < 16; j++) to[j] = *reinterpret_cast<const u32_any*>(x_base + (u64)idx[j] * ct_stride);
+        for (int k = 0; k < 8; k++) to[k] = *reinterpret_cast<const u32x4*>(x_base + (u64)idx[k] * ct_stride);
     };
-    auto request_w = [&](u32 b) {
+    auto request_w = [&](u32 block, v4i (&to)[OT]) {
 #pragma unroll
-        for (int o = 0; o < OT; o++) w[o] = table[((size_t)min(b, blocks - 1) * OT + o) * 64];
+        for (int o = 0; o < OT; o++) to[o] = table[((size_t)min(block, blocks - 1) * (2 * OT) + o) * 64];
     };
-    auto multiply = [&](u32 (&from)[16], u32 b) {
-        v4i in[ND];
+    // one half of the digits of column tile k: eight terms
+    auto write_operand = [&](v4i* to, const u32x4 (&from)[8], int k, int h) {
+        u32 t[2][ND];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            u32 t[ND];
-            transpose4<ND>(from[4 * j], from[4 * j + 1], from[4 * j + 2], from[4 * j + 3], t);
-#pragma unroll
-            for (int d = 0; d < ND; d++) in[d][j] = (int)t[d];
+        for (int j = 0; j < 2; j++) {
+            auto bytes = [&](int i) -> u32 {  // the second half's start at byte ND
+                const u32 lo = from[i][2 * k], hi = from[i][2 * k + 1];
+                return h == 0 ? lo : ND == 4 ? hi : __builtin_amdgcn_alignbyte(hi, lo, ND);
+            };
+            transpose4<ND>(bytes(4 * j), bytes(4 * j + 1), bytes(4 * j + 2), bytes(4 * j + 3), t[j]);
         }
-        v4i now[OT];
 #pragma unroll
-        for (int o = 0; o < OT; o++) now[o] = w[o];
-        request_w(b + 1);
-        request_x(from);
-        request_idx(b + 3);
-#pragma unroll
-        for (int o = 0; o < OT; o++)
-#pragma unroll
-            for (int d = 0; d < ND; d++) sums[o][d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now[o], in[d], sums[o][d], 0, 0, 0);
-    };
-    if (blocks) {
-        request_idx(0);
-        request_w(0);
-        request_x(x[0]);
-        request_idx(1);
-        request_x(x[1]);
-        request_idx(2);
-        u32 b = 0;
-        for (; b + 1 < blocks; b += 2) {
-            multiply(x[0], b);
-            multiply(x[1], b + 1);
+        for (int d = 0; d < ND; d++) {
+            u32x2* p = reinterpret_cast<u32x2*>(to + ((load_block * 8 + h * ND + d) * 2 + k) * 64 + load_half * 32 + col) + half;
+            *p = u32x2{t[0][d], t[1][d]};
         }
-        if (b < blocks) multiply(x[0], b);
-    }
-
-    const End<V> fin = end_of(a, c, limb_const, row, slot);
-    const size_t out_stride = (size_t)2 * a.limbs * a.N;
-    V* const dst = a.out + g.out0 * out_stride + at;
-    auto output_of = [&](int o, int r) -> u32 { return 32 * o + 8 * (r / 4) + 4 * half + r % 4; };
-    auto sum = [&](int o, int r) {
-        return fin.template half<ND>(sums[o][0][r], sums[o][1][r], ND > 2 ? sums[o][ND > 2 ? 2 : 0][r] : 0, ND > 3 ? sums[o][ND > 3 ? 3 : 0][r] : 0);
     };
-    auto store = [&](u32 o, u64 r) {
-        if (o >= g.count) return;
-        const Ends e = ends[o];
-        u64 v = fin.finish(r, e.channel, e.bias, 0);
-        V* const p = dst + o * out_stride;
-        if (fin.accumulate) v = add_mod(v, *p, fin.q);
-        *p = (V)v;
-    };
-    if constexpr (sizeof(V) == 8) {
-        // of every tile the wavefront of the lower digits finishes the first eight of a lane's outputs, the other one the last eight
-        auto finish = [&](auto of_upper) {
-            constexpr bool UPPER = decltype(of_upper)::value;
-            constexpr int KEEP = UPPER ? 8 : 0, SEND = 8 - KEEP;
+    auto multiply = [&](auto of_parity, u32 s) {
+        constexpr int P = decltype(of_parity)::value;
+        const v4i* from = lds + P * OPERAND_PIECES + lane;
+        v4i* to = lds + (P ^ 1) * OPERAND_PIECES;
+        lds_barrier();  // the operands of this step are in place, and nobody reads the others any more
 #pragma unroll
-            for (int o = 0; o < OT; o++) {
-                if (32 * (u32)o >= g.count) break;
-                u64* buf = exchange + (o & 1) * (WAVES * 8 * 64) + lane;
+        for (int q = 0; q < 4; q++) {  // block q / 2, column tile q % 2; a fourth of the next step's operands
+            if (q < 2 || 2 * s + 1 < blocks) {
 #pragma unroll
-                for (int k = 0; k < 8; k++) buf[(wave * 8 + k) * 64] = sum(o, SEND + k);
-                lds_barrier();  // (also for the ends)
+                for (int d = 0; d < ND; d++) {
+                    const v4i in = from[((q / 2 * 8 + upper * ND + d) * 2 + q % 2) * 64];
 #pragma unroll
-                for (int k = 0; k < 8; k++) {
-                    const u64 mine = sum(o, KEEP + k), other = buf[((wave ^ 1) * 8 + k) * 64];
-                    store(output_of(o, KEEP + k), UPPER ? fin.join(other, mine) : fin.join(mine, other));
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int o = 0; o < OT; o++)
+                        sums[o][q % 2][d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q / 2][o], in, sums[o][q % 2][d], 0, 0, 0);
                 }
             }
-        };
-        if (upper) finish(std::true_type{});
-        else finish(std::false_type{});
-    } else {
-        lds_barrier();
+            if (q % 2) request_w(2 * s + 2 + q / 2, w[q / 2]);
+            write_operand(to, x[(P ^ 1) % AHEAD], q % 2, q / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        request_x(x[(P ^ 1) % AHEAD]);
+        request_idx(s + AHEAD + 2);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (blocks) {
+        const u32 steps = (blocks + 1) / 2;
+        request_w(0, w[0]);
+        request_w(1, w[1]);
+        request_idx(0);
+        request_x(x[0]);
+        request_idx(1);
+        if constexpr (AHEAD == 2) {
+            request_x(x[1]);
+            request_idx(2);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) write_operand(lds, x[0], q % 2, q / 2);
+        request_x(x[0]);
+        request_idx(AHEAD + 1);
+        u32 s = 0;
+        for (; s + 1 < steps; s += 2) {
+            multiply(std::integral_constant<int, 0>{}, s);
+            multiply(std::integral_constant<int, 1>{}, s + 1);
+        }
+        if (s < steps) multiply(std::integral_constant<int, 0>{}, s);
+        lds_barrier();  // (the operands are not read any more)
+    }
+
+    const End<V, 2> fin = end_of<V, 2>(a, c, limb_const, row, slot);
+    const size_t out_stride = (size_t)2 * a.limbs * a.N;
+    V* const dst = a.out + g.out0 * out_stride + at;
+    auto sum = [&](int o, int k, int r) {
+        const v16i (&t)[ND] = sums[o][k];
+        return fin.template half<ND>(t[0][r], t[1][r], ND > 2 ? t[ND > 2 ? 2 : 0][r] : 0, ND > 3 ? t[ND > 3 ? 3 : 0][r] : 0);
+    };
+    // Of every tile the wavefront of the lower digits finishes the first eight of a lane's outputs, the other one the last eight: they exchange the
+    // others' sums.
+    auto finish = [&](auto of_upper) {
+        constexpr bool UPPER = decltype(of_upper)::value;
+        constexpr int KEEP = UPPER ? 8 : 0, SEND = 8 - KEEP;
+        u64* exchange = reinterpret_cast<u64*>(lds) + lane;  // [tile parity][wavefront][output][column tile][lane]
 #pragma unroll
         for (int o = 0; o < OT; o++) {
-            if (32 * (u32)o >= g.count) break;
+            u64* buf = exchange + (o & 1) * (WAVES * 16 * 64);
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                store(output_of(o, r), sum(o, r));
+            for (int i = 0; i < 16; i++) buf[(wave * 16 + i) * 64] = sum(o, i % 2, SEND + i / 2);
+            lds_barrier();  // (also for the ends)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const u32 r = KEEP + i, mine = 32 * (tile0 + o) + 8 * (r / 4) + 4 * half + r % 4;
+                if (mine < g.count) {
+                    const Ends e = ends[mine];
+                    V* const p = dst + mine * out_stride;
+                    u64 own_sum[2], other[2];
+#pragma unroll
+                    for (int k = 0; k < 2; k++) own_sum[k] = sum(o, k, KEEP + i), other[k] = buf[((wave ^ 1) * 16 + 2 * i + k) * 64];
+                    fin.store(p, e, UPPER ? other : own_sum, UPPER ? own_sum : other);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-    }
+    };
+    if (upper) finish(std::true_type{});
+    else finish(std::false_type{});
 }
 
 template <typename V, int OT>
-__global__ void __launch_bounds__(THREADS, OT == 2 ? 2 : 1) i8_split_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
-    __shared__ Ends ends[32 * OT];
-    __shared__ u64 exchange[sizeof(V) == 8 ? 2 * WAVES * 8 * 64 : 1];
+__global__ void __launch_bounds__(THREADS, OT == 1 ? 2 : 1) i8_split_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
+    __shared__ Ends ends[64 * OT];
+    __shared__ v4i lds[2 * OPERAND_PIECES];
     const Place at = place_of(a.N / split_slots<V>(), a.runs);
     const I8Group g = load_group(a.groups + a.first + at.run);
     const LimbConst& c = lt.c[at.row >> 1];
     const I8Limb& l = lc.c[at.row >> 1];
-    if constexpr (sizeof(V) == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, exchange);
-    else if (l.nd == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, exchange);
-    else if (l.nd == 3) split_body<V, OT, 3>(a, c, l, g, at.part, at.row, ends, exchange);
-    else split_body<V, OT, 2>(a, c, l, g, at.part, at.row, ends, exchange);
+    if constexpr (sizeof(V) == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, lds);
+    else if (l.nd == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, lds);
+    else if (l.nd == 3) split_body<V, OT, 3>(a, c, l, g, at.part, at.row, ends, lds);
+    else split_body<V, OT, 2>(a, c, l, g, at.part, at.row, ends, lds);
 }
 
 template <typename V>
@@ -489,15 +517,15 @@ u64 class_blocks(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls, u3
     return (count + *run - 1) / *run * parts * rows;
 }
 
-template <typename V, int OT>
+template <typename V, int CLS>
 int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) {
-    a.first = l->class_begin[OT - 1];
-    a.n_groups = class_count<V>(l, OT - 1);
+    a.first = l->class_begin[CLS];
+    a.n_groups = class_count<V>(l, CLS);
     if (a.n_groups == 0) return HE_OK;
-    const dim3 grid((u32)class_blocks<V>(ctx, l, a.limbs, OT - 1, &a.run)), block(THREADS);
+    const dim3 grid((u32)class_blocks<V>(ctx, l, a.limbs, CLS, &a.run)), block(THREADS);
     a.runs = (a.n_groups + a.run - 1) / a.run;
-    if constexpr (OT == 1) hipLaunchKernelGGL(i8_whole_kernel<V>, grid, block, 0, s, ctx->limbs, l->limbs, a);
-    else hipLaunchKernelGGL((i8_split_kernel<V, OT>), grid, block, 0, s, ctx->limbs, l->limbs, a);
+    if constexpr (CLS == 0) hipLaunchKernelGGL(i8_whole_kernel<V>, grid, block, 0, s, ctx->limbs, l->limbs, a);
+    else hipLaunchKernelGGL((i8_split_kernel<V, CLS>), grid, block, 0, s, ctx->limbs, l->limbs, a);
     HE_HIP(hipGetLastError());
     return HE_OK;
 }
@@ -507,10 +535,9 @@ int launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const V* ct_in, const V
     const I8Args<V> a{l->groups_dev, l->lists_dev, reinterpret_cast<const v4i*>(l->table_dev), sizeof(V) == 8 ? l->channels_dev : l->channels32_dev,
                       ct_in, token, bias, out, limbs, ctx->N, l->n_out, 0, 0, 0, 0, accumulate};
     int rc;
+    if ((rc = launch_class<V, 0>(ctx, a, l, s)) != HE_OK) return rc;
     if ((rc = launch_class<V, 1>(ctx, a, l, s)) != HE_OK) return rc;
-    if ((rc = launch_class<V, 2>(ctx, a, l, s)) != HE_OK) return rc;
-    if ((rc = launch_class<V, 3>(ctx, a, l, s)) != HE_OK) return rc;
-    return launch_class<V, 4>(ctx, a, l, s);
+    return launch_class<V, 2>(ctx, a, l, s);
 }
 
 u64 mul_mod_host(u64 a, u64 b, u64 q) { return (u64)((u128)a * b % q); }
@@ -546,12 +573,14 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
         u32 end = o + 1;
         while (end < n_out && rows.same_inputs(o, end)) end++;
         const u32 terms = rows.terms(o), blocks = (terms + 31) / 32;
-        // (outputs without terms go to the second form, whose loop over the blocks may be empty)
-        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + I8_CLASSES - 1) / I8_CLASSES, per = std::max((tiles + cuts - 1) / cuts, terms ? 1u : 2u);
+        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + 3) / 4, each = (tiles + cuts - 1) / cuts * 32;
         const u32 list = (u32)(h.lists.size() / 32);
         for (u32 t = 0; t < blocks * 32; t++) h.lists.push_back(term_ct[off[o] + std::min(t, terms - 1)]);
-        for (; o < end; o += std::min(per * 32, end - o)) {
-            I8Group g{o, std::min(per * 32, end - o), terms, list, 0, {0, 0, 0}};
+        for (u32 count; o < end; o += count) {
+            count = std::min(each, end - o);
+            I8Group g{o, count, terms, list, 0, {0, 0, 0}};
+            // (outputs without terms go to the second form, whose loop over the blocks may be empty)
+            const u32 cls = count > 64 ? 2 : count > 32 || terms == 0 ? 1 : 0, per = 1u << cls;
             const size_t n = (size_t)g.count * terms;  // the plaintexts of a group's outputs follow one another
             u64 hash = 0xCBF29CE484222325ull ^ n;
             for (size_t i = 0; i < n; i++) hash = (hash ^ term_pt[off[o] + i]) * 0x100000001B3ull;
@@ -573,7 +602,7 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
                         t0[(((size_t)t / 32 * per + r / 32) * 64 + t % 32 / 16 * 32 + r % 32) * 16 + t % 16] = weights[term_pt[off[o + r] + t]];
                 known.emplace(hash, g);
             }
-            classes[per - 1].push_back(g);
+            classes[cls].push_back(g);
         }
     }
     for (u32 cls = 0; cls < I8_CLASSES; cls++) {

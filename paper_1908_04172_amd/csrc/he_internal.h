@@ -151,7 +151,7 @@ struct he_plan {
 };
 
 // ---- int8 layers (he_i8.hip)
-constexpr u32 I8_CLASSES = 4;          // groups of up to 32, 64, 96 and 128 outputs
+constexpr u32 I8_CLASSES = 3;          // groups of up to 32, 64 and 128 outputs
 constexpr u32 I8_MAX_TERMS = 131071;   // of an output: sums of so many products of at most 2^14 stay below 2^31
 // Outputs that read the same ciphertexts in the same order.
 struct I8Group {
