@@ -372,6 +372,75 @@ HE_HD u32 digit_reduce32(const int32_t (&r)[4], u32 start, const DigitConst& c) 
 }
 
 // ---------------------------------------------------------------------------------------------
+// Sums of products with 8-bit integer weights (he_i8.hip).  A residue's bytes x_d (2 nd of them, nd = 2, 3 or 4) enter the matrix cores as the
+// signed digits x_d - 128; with S_d = sum_t w_t (x_td - 128) a sum is
+//   sum_t w_t x_t = y0 + 256^nd y1 + F sum_t w_t - (1 + 256^nd) 2^56,   F = 128 sum_(d < 2 nd) 256^d,
+//   y0 = 2^56 + sum_(d < nd) 256^d S_d,   y1 = 2^56 + sum_(d < nd) 256^d S_(nd + d),
+// and y0, y1 lie between 0 and 2^57: |S_d| < 2^31 for up to 131071 terms, so the sums are below 2^55.1 in magnitude.  An
+// output s * sum is y0 s0 + y1 s1 + addend modulo q, with s0 = s, s1 = s 256^nd and all the rest in the addend: two products by
+// constants that share one quotient estimate.
+constexpr int I8_OFFSET_BITS = 56;
+struct I8Limb {
+    u64 q, two_q;
+    u32 nd;
+    u32 exact;       // 1: q >= 2^60, where the estimate must be the exact one
+    u32 bits_shift;  // bit length of q, minus 8
+    u32 mult;        // floor(2^(16 + bits_shift) / q)
+};
+struct I8Channel {
+    u64 s0, s0_shoup, s1, s1_shoup, addend;
+};
+
+HE_HD u32 min_u32(u32 a, u32 b) { return a < b ? a : b; }
+
+// Congruent to y0 s0 + y1 s1 + addend.  With the cheap estimates (each short by at most 2, and the products' companions by 1) below
+// 4q + 4q + q, which fits 64 bits for q < 2^60; else each product is taken below 2q, and the result is below 3q.
+HE_HD u64 i8_combine(u64 y0, u64 y1, const I8Channel& ch, const I8Limb& c) {
+    if (c.exact) {
+        const u64 v = shoup_mul_lazy(y0, ch.s0, ch.s0_shoup, c.q) + shoup_mul_lazy(y1, ch.s1, ch.s1_shoup, c.q);
+        return (v >= c.two_q ? v - c.two_q : v) + ch.addend;
+    }
+    const u64 qh = shoup_quotient_cheap(y0, ch.s0_shoup) + shoup_quotient_cheap(y1, ch.s1_shoup), nq = 0 - c.q;
+    u64 cross = mad_wide((u32)y0, (u32)(ch.s0 >> 32), 0);
+    cross = mad_wide((u32)(y0 >> 32), (u32)ch.s0, cross);
+    cross = mad_wide((u32)y1, (u32)(ch.s1 >> 32), cross);
+    cross = mad_wide((u32)(y1 >> 32), (u32)ch.s1, cross);
+    cross = mad_wide((u32)qh, (u32)(nq >> 32), cross);
+    cross = mad_wide((u32)(qh >> 32), (u32)nq, cross);
+    u64 e = (u64)(u32)y0 * (u32)ch.s0 + ch.addend;
+    e = (u64)(u32)y1 * (u32)ch.s1 + e;
+    e = (u64)(u32)qh * (u32)nq + e;
+    u32 hi = (u32)(e >> 32) + (u32)cross;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm("" : "+v"(hi));  // (see shoup_remainder_add)
+#endif
+    return ((u64)hi << 32) | (u32)e;
+}
+
+// The canonical residue of v below 9q (3q for q >= 2^60): the quotient from the upper bits of v, below 9 * 2^8, is short by at most
+// one (v's lower bits are worth 2^-7, the multiplier's rounding at most 9 * 2^-8).
+HE_HD u64 i8_reduce(u64 v, const I8Limb& c) {
+    const u32 k = ((u32)(v >> c.bits_shift) * c.mult) >> 16;
+    return sub_if_ge(v - (u64)k * c.q, 0 - c.q);
+}
+
+// The same in packed storage (q < 2^30): a residue has one half, y s0 + addend.  The estimate of 64 bits leaves a product below 4q < 2^32, of
+// which the low words suffice.
+HE_HD u32 i8_finish32(u64 y, const I8Channel& ch, const I8Limb& c) {
+    const u32 q = (u32)c.q;
+    u32 v = (u32)y * (u32)ch.s0 - (u32)shoup_quotient_cheap(y, ch.s0_shoup) * q;
+    v = min_u32(v, v - 2 * q);  // (the difference wraps to a larger number exactly when v < 2q)
+    v += (u32)ch.addend;        // below 3q
+    v = min_u32(v, v - 2 * q);
+    return min_u32(v, v - q);
+}
+
+// ... and of tok * v + bias, tok with its Shoup companion
+HE_HD u64 i8_token(u64 v, u64 tok, u64 tok_shoup, u64 bias, const I8Limb& c) {
+    return i8_reduce(shoup_remainder_add(v, tok, shoup_quotient(v, tok_shoup), c.q, bias), c);  // below 3q
+}
+
+// ---------------------------------------------------------------------------------------------
 // 32-bit moduli (below 2^30), the primitives of the packed path.
 
 // Alg. 6 (BarrettReduction64): z mod q for a 64-bit z, ratio = floor(2^64 / q).  The estimate

@@ -11,14 +11,13 @@
 // v_mfma_i32_32x32x32_i8 takes 32 terms times 32 outputs times 32 slots of one digit.  A lane's share of the input operand is one byte of 16
 // terms at one slot: it loads the bytes of each of the 16 residues and transposes them in registers (4 x 4 bytes: eight byte
 // permutations).  The digits go in two halves, bytes 0 .. ND-1 and ND .. 2 ND-1 (ND = 2, 3 or 4 by the modulus), in one of two forms:
-//  - groups of up to 32 outputs (convolutions, narrow layers): a wavefront takes both halves of 32 slots and runs through several
-//    groups, the inputs of the next block of terms in flight; wavefronts never meet;
-//  - larger ones: a wavefront takes one half, which leaves room for the sums of up to 128 outputs, so that the inputs are read
-//    once for so many; the two wavefronts of a slot exchange half of their results at the end.
+//  - groups of up to 32 outputs (convolutions, narrow layers), with v_mfma_i32_16x16x32_i8 in the same manner: a wavefront takes both halves of 32 slots
+//    and runs through several groups, the inputs of the next block of terms in flight; wavefronts never meet;
+//  - larger ones: a workgroup shares the operands of 64 slots among four wavefronts, one for each half and 32 outputs, which exchange half of
+//    their results at the end.
 // Residues in packed storage are taken two at a time as one of eight bytes (first form), or one half alone (second).
 //
-// The end of an output: with y0, y1 the halves' sums, |y| < 2^55.1, each plus 2^56, r = y0 + (y1 256^ND mod q) is one Shoup product, and
-// r s_o another, whose result is below 2q; what the offsets, the flipped bits and s_o leave to add is a constant of the output and limb.
+// The end of an output, two products by constants of the output and one reduction: I8Channel in he_arith.h.
 #include <string.h>
 
 #include <algorithm>
@@ -34,13 +33,11 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 constexpr u32 THREADS = 256, WAVES = THREADS / 64;
-constexpr int OFFSET_BITS = 56;      // what makes a half of a sum positive
 constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most
 constexpr u64 MIN_WORKGROUPS = 2048; // ... while the launch keeps at least this many workgroups
+constexpr u64 SMALL_LAUNCH = 512;    // workgroups
 
-// slots of a workgroup: 32 units of eight bytes per wavefront in the first form, 64 in all in the second
-template <typename V>
-__host__ __device__ constexpr u32 whole_slots() { return 32 * WAVES * 8 / sizeof(V); }
+// slots of 64 units of eight bytes, a workgroup of the second form
 template <typename V>
 __host__ __device__ constexpr u32 split_slots() { return 64 * 8 / sizeof(V); }
 
@@ -102,71 +99,61 @@ __device__ __forceinline__ u64 shoup_companion(u64 w, const LimbConst& c) {
 
 // What the end of an output reads from the LDS.  Without tokens the bias is part of the addend.
 struct Ends {
-    u64 s, s_shoup, addend, bias;
+    I8Channel ch;
+    u64 bias;
 };
 template <typename V>
-__device__ __forceinline__ Ends ends_of(const I8Args<V>& a, const LimbConst& c, u32 row, u32 output) {
-    const I8Channel ch = a.channels[(size_t)(row >> 1) * a.n_out + output];
-    const u64 bias = a.bias && !(row & 1) ? a.bias[(size_t)output * a.limbs + (row >> 1)] : 0;
-    return Ends{ch.s, ch.s_shoup, a.token ? ch.addend : add_mod(ch.addend, bias, c.q), bias};
+__device__ __forceinline__ Ends ends_of(const I8Args<V>& a, u32 row, u32 output, u64 q) {
+    Ends e{a.channels[(size_t)(row >> 1) * a.n_out + output], a.bias && !(row & 1) ? a.bias[(size_t)output * a.limbs + (row >> 1)] : 0};
+    if (!a.token) e.ch.addend = add_mod(e.ch.addend, e.bias, q);
+    return e;
 }
 
-// What the ends of all outputs of a row have in common.
-template <typename V, int UNITS>
+// What the ends of all outputs of a row have in common, for two neighbouring units of eight bytes per lane.
+template <typename V>
 struct End {
-    static constexpr int SLOTS = UNITS * 8 / sizeof(V);
-    u64 q, two_q;
-    I8Limb limb;
+    static constexpr int SLOTS = 16 / sizeof(V);
+    I8Limb c;
     u64 tok[SLOTS], tok_shoup[SLOTS];  // the tokens of this lane's slots
     bool has_token, accumulate;
-    int32_t b8, b16, b24;     // 2^8, 2^16, 2^24 as data (multiplied by a literal they become shifts and additions)
+    int32_t b8, b16, b24;              // 2^8, 2^16, 2^24 as data (multiplied by a literal they become shifts and additions)
 
     // the sum of one half's digits, made positive
-    template <int ND>
-    __device__ __forceinline__ u64 half(int32_t s0, int32_t s1, int32_t s2, int32_t s3) const {
-        int64_t v = (int64_t)(1ull << OFFSET_BITS) + (int64_t)s0;
-        v = (int64_t)s1 * b8 + v;
-        if constexpr (ND > 2) v = (int64_t)s2 * b16 + v;
-        if constexpr (ND > 3) v = (int64_t)s3 * b24 + v;
-        return (u64)v;
-    }
-    // both halves -> what the channel's scale multiplies: a 64-bit value congruent to the sum, below 4q + 2^57 for q < 2^61, else 2q + 2^57
-    __device__ __forceinline__ u64 join(u64 y0, u64 y1) const {
-        return shoup_remainder_add(y1, limb.shift, limb.cheap ? shoup_quotient_cheap(y1, limb.shift_shoup) : shoup_quotient(y1, limb.shift_shoup), q, y0);
-    }
-    // the residue of an output
-    __device__ __forceinline__ u64 finish(u64 r, const Ends& e, int k) const {
-        u64 v = shoup_remainder_add(r, e.s, shoup_quotient(r, e.s_shoup), q, e.addend);  // below 3q
-        if (has_token) {
-            v = shoup_remainder_add(v, tok[k], shoup_quotient(v, tok_shoup[k]), q, e.bias);
-        }
-        v = v >= two_q ? v - two_q : v;
-        return v >= q ? v - q : v;
-    }
-    // an output at UNITS neighbouring units, from the sums of their halves
-    __device__ __forceinline__ void store(V* p, const Ends& e, const u64 (&y0)[UNITS], const u64 (&y1)[UNITS]) const {
-        typedef V piece __attribute__((ext_vector_type(SLOTS), aligned(8)));
+    __device__ __forceinline__ u64 half(int32_t s0, int32_t s1) const { return (u64)((int64_t)s1 * b8 + ((int64_t)(1ull << I8_OFFSET_BITS) + (int64_t)s0)); }
+    __device__ __forceinline__ u64 half(int32_t s0, int32_t s1, int32_t s2) const { return (u64)((int64_t)s2 * b16 + (int64_t)half(s0, s1)); }
+    __device__ __forceinline__ u64 half(int32_t s0, int32_t s1, int32_t s2, int32_t s3) const { return (u64)((int64_t)s3 * b24 + (int64_t)half(s0, s1, s2)); }
+
+    // an output, from the sums of its halves at the two units
+    __device__ __forceinline__ void store(V* p, const Ends& e, const u64 (&y0)[2], const u64 (&y1)[2]) const {
+        typedef V piece __attribute__((ext_vector_type(SLOTS), aligned(8)));  // 16 bytes (see u64x2)
         piece v;
 #pragma unroll
-        for (int k = 0; k < UNITS; k++) {
-            if constexpr (sizeof(V) == 8) v[k] = finish(join(y0[k], y1[k]), e, k);
-            else v[2 * k] = (V)finish(y0[k], e, 2 * k), v[2 * k + 1] = (V)finish(y1[k], e, 2 * k + 1);
+        for (int k = 0; k < 2; k++) {
+            if constexpr (sizeof(V) == 8) {
+                const u64 r = i8_combine(y0[k], y1[k], e.ch, c);
+                v[k] = has_token ? i8_token(r, tok[k], tok_shoup[k], e.bias, c) : i8_reduce(r, c);
+            } else {  // the halves are two slots
+                v[2 * k] = i8_finish32(y0[k], e.ch, c);
+                v[2 * k + 1] = i8_finish32(y1[k], e.ch, c);
+                if (has_token) {
+                    v[2 * k] = (u32)i8_token(v[2 * k], tok[2 * k], tok_shoup[2 * k], e.bias, c);
+                    v[2 * k + 1] = (u32)i8_token(v[2 * k + 1], tok[2 * k + 1], tok_shoup[2 * k + 1], e.bias, c);
+                }
+            }
         }
         if (accumulate) {
             const piece old = *reinterpret_cast<const piece*>(p);
 #pragma unroll
-            for (int k = 0; k < SLOTS; k++) v[k] = (V)add_mod(v[k], old[k], q);
+            for (int k = 0; k < SLOTS; k++) v[k] = (V)add_mod(v[k], old[k], c.q);
         }
         *reinterpret_cast<piece*>(p) = v;
     }
 };
 
-template <typename V, int UNITS>
-__device__ __forceinline__ End<V, UNITS> end_of(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb, u32 row, u32 slot) {
-    End<V, UNITS> e;
-    e.q = c.q;
-    e.two_q = c.two_q;
-    e.limb = limb;
+template <typename V>
+__device__ __forceinline__ End<V> end_of(const I8Args<V>& a, const LimbConst& lc, const I8Limb& limb, u32 row, u32 slot) {
+    End<V> e;
+    e.c = limb;
     e.has_token = a.token != nullptr;
     e.accumulate = a.accumulate;
     e.b8 = 1 << 8;
@@ -178,14 +165,22 @@ __device__ __forceinline__ End<V, UNITS> end_of(const I8Args<V>& a, const LimbCo
         e.tok[k] = e.tok_shoup[k] = 0;
         if (e.has_token) {
             e.tok[k] = a.token[(size_t)(row >> 1) * a.N + slot + k];
-            e.tok_shoup[k] = shoup_companion(e.tok[k], c);
+            e.tok_shoup[k] = shoup_companion(e.tok[k], lc);
         }
     }
     return e;
 }
 
+// The half of the digits (bytes 0 .. ND - 1, or ND .. 2 ND - 1) of unit k of a lane's 16 bytes
+template <int ND>
+__device__ __forceinline__ u32 half_bytes(const u32x4& x, int k, int half) {
+    return half == 0 ? x[2 * k] : ND == 4 ? x[2 * k + 1] : __builtin_amdgcn_alignbyte(x[2 * k + 1], x[2 * k], ND);
+}
+
 // ---------------------------------------------------------------------------------------------
-// First form: up to 32 outputs.
+// First form: up to 32 outputs, RT tiles of 16.  A lane loads 16 bytes (units 2 l and 2 l + 1 of the wavefront's 32, l = lane % 16) of the eight
+// terms of its quarter of a block (lane / 16); unit 2 l + k is column l of column tile k.  Of a result tile a lane holds the rows 4 (lane / 16) ..: row
+// 4 i + r is output 4 r + i of the tile, so that few outputs are spread over all lanes.
 
 struct Cursor {
     u32 group, block, blocks;
@@ -208,91 +203,108 @@ __device__ __forceinline__ void step(Cursor& c, const I8Args<V>& a, u32 end) {  
     else if (c.group + 1 < end) c = enter(a, c.group + 1);
 }
 
-template <typename V, int ND>
-__device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb_const, u32 part, u32 row, u32 begin, u32 end, Ends* lds) {
-    const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
-    constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit of eight bytes
+template <typename V, int RT, int ND>
+__device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& lc, const I8Limb& limb_const, u32 part, u32 row, u32 begin, u32 end, Ends* lds) {
+    const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64, quarter = lane / 16, col = lane % 16;
+    constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit
     const u32 comp = row & 1, limb = row >> 1;
-    const u32 slot = part * whole_slots<V>() + (wave * 32 + lane % 32) * PER;
+    const u32 slot = (part * blockDim.x / 2 + wave * 32 + col * 2) * PER;
     const size_t at = ((size_t)comp * a.limbs + limb) * a.N + slot;
     const u32 ct_stride = 2 * a.limbs * a.N * sizeof(V);     // bytes
     const char* x_base = reinterpret_cast<const char*>(a.ct_in + at);
     const size_t out_stride = (size_t)2 * a.limbs * a.N;
     V* const dst0 = a.out + at;
-    for (u32 i = threadIdx.x; i < (end - begin) * 32; i += THREADS) {
-        const I8Group& g = a.groups[a.first + begin + i / 32];
-        if (i % 32 < g.count) lds[i] = ends_of(a, c, row, g.out0 + i % 32);
+    for (u32 i = threadIdx.x; i < (end - begin) * 16 * RT; i += blockDim.x) {
+        const I8Group& g = a.groups[a.first + begin + i / (16 * RT)];
+        if (i % (16 * RT) < g.count) lds[i] = ends_of(a, row, g.out0 + i % (16 * RT), lc.q);
     }
-    const End<V, 1> fin = end_of<V, 1>(a, c, limb_const, row, slot);
+    const End<V> fin = end_of(a, lc, limb_const, row, slot);
     __syncthreads();
 
     Cursor cur = enter(a, begin), nxt = cur;
     step(nxt, a, end);
     Cursor after = nxt;
     step(after, a, end);
-    u32 idx[16];
-    u32x2 x[16];
-    v4i w, w_next;
-    auto request_idx = [&](const Cursor& p, int j) {  // four terms
-        const u32x4 v = *reinterpret_cast<const u32x4*>(a.lists + (size_t)(p.list + p.block) * 32 + half * 16 + 4 * j);
+    u32 idx[8];
+    u32x4 x[8];
+    u64 w[RT], w_next[RT];
+    auto request_idx = [&](const Cursor& p) {
 #pragma unroll
-        for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
+        for (int j = 0; j < 2; j++) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(a.lists + (size_t)(p.list + p.block) * 32 + quarter * 8 + 4 * j);
+#pragma unroll
+            for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
+        }
     };
-    auto request_x = [&](int j) {
+    auto request_x = [&] {
 #pragma unroll
-        for (int k = 4 * j; k < 4 * j + 4; k++) x[k] = *reinterpret_cast<const u32x2*>(x_base + (u64)idx[k] * ct_stride);
+        for (int k = 0; k < 8; k++) x[k] = *reinterpret_cast<const u32x4*>(x_base + (u64)idx[k] * ct_stride);
     };
-    auto request_w = [&](const Cursor& p) { return a.table[(size_t)(p.table + p.block) * 64 + lane]; };
-    w = request_w(cur);
+    auto request_w = [&](const Cursor& p, u64 (&to)[RT]) {
 #pragma unroll
-    for (int j = 0; j < 4; j++) request_idx(cur, j);
-#pragma unroll
-    for (int j = 0; j < 4; j++) request_x(j);
-#pragma unroll
-    for (int j = 0; j < 4; j++) request_idx(nxt, j);
-    v16i sums[2 * ND];
+        for (int o = 0; o < RT; o++) to[o] = reinterpret_cast<const u64*>(a.table)[((size_t)p.table + p.block * RT + o) * 64 + lane];
+    };
+    request_idx(cur);
+    request_w(cur, w);
+    request_x();
+    request_idx(nxt);
+    v4i sums[RT][2][2 * ND];
     while (true) {
-        const bool first = cur.block == 0, last = cur.block + 1 == cur.blocks;
-        if (first) {
+        const bool last = cur.block + 1 == cur.blocks;
+        if (cur.block == 0) {
+#pragma unroll
+            for (int o = 0; o < RT; o++)
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+#pragma unroll
+                    for (int d = 0; d < 2 * ND; d++) sums[o][k][d] = v4i{0, 0, 0, 0};
+        }
+        request_w(nxt, w_next);
+        u64 in[2][2 * ND];
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                u32 t[2][ND];
+#pragma unroll
+                for (int j = 0; j < 2; j++)
+                    transpose4<ND>(half_bytes<ND>(x[4 * j], k, h), half_bytes<ND>(x[4 * j + 1], k, h), half_bytes<ND>(x[4 * j + 2], k, h),
+                                   half_bytes<ND>(x[4 * j + 3], k, h), t[j]);
+#pragma unroll
+                for (int d = 0; d < ND; d++) in[k][h * ND + d] = (u64)t[1][d] << 32 | t[0][d];
+            }
+        request_x();
+        request_idx(after);
+#pragma unroll
+        for (int k = 0; k < 2; k++)
 #pragma unroll
             for (int d = 0; d < 2 * ND; d++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) sums[d][i] = 0;
-        }
-        v4i in[2 * ND];
-        w_next = request_w(nxt);
+                for (int o = 0; o < RT; o++)
+                    sums[o][k][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)w[o], (long)in[k][d], sums[o][k][d], 0, 0, 0);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {  // (four terms at a time, whose registers take those of the next block)
-            u32 lo[ND], hi[ND];
-            // the second half's bytes start at byte ND
-            auto up = [&](int k) -> u32 { return ND == 4 ? x[k][1] : __builtin_amdgcn_alignbyte(x[k][1], x[k][0], ND); };
-            transpose4<ND>(x[4 * j][0], x[4 * j + 1][0], x[4 * j + 2][0], x[4 * j + 3][0], lo);
-            transpose4<ND>(up(4 * j), up(4 * j + 1), up(4 * j + 2), up(4 * j + 3), hi);
-#pragma unroll
-            for (int d = 0; d < ND; d++) in[d][j] = (int)lo[d], in[ND + d][j] = (int)hi[d];
-            request_x(j);
-            request_idx(after, j);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int d = 0; d < 2 * ND; d++) sums[d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, in[d], sums[d], 0, 0, 0);
-        w = w_next;
+        for (int o = 0; o < RT; o++) w[o] = w_next[o];
         if (last) {
             const I8Group g = load_group(a.groups + a.first + cur.group);
-            const Ends* ends = lds + (cur.group - begin) * 32;
+            const Ends* ends = lds + (cur.group - begin) * 16 * RT;
             V* const dst = dst0 + g.out0 * out_stride;
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                if (8 * (u32)(r / 4) >= g.count) break;      // (rows of both halves)
-                const u32 o = 8 * (r / 4) + 4 * half + r % 4;
-                if (o < g.count) {
-                    const Ends e = ends[o];
-                    auto sum = [&](int h) {
-                        return fin.template half<ND>(sums[h * ND][r], sums[h * ND + 1][r], ND > 2 ? sums[h * ND + (ND > 2 ? 2 : 0)][r] : 0,
-                                                     ND > 3 ? sums[h * ND + (ND > 3 ? 3 : 0)][r] : 0);
-                    };
-                    const u64 y0[1] = {sum(0)}, y1[1] = {sum(1)};
-                    fin.store(dst + o * out_stride, e, y0, y1);
+            for (int i = 0; i < 4 * RT; i++) {
+                if (4 * (u32)i >= g.count) break;
+                const u32 mine = 4 * i + quarter;
+                if (mine < g.count) {
+                    u64 y[2][2];
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int k = 0; k < 2; k++) {
+                            const v4i (&t)[2 * ND] = sums[i / 4][k];
+                            const int r = i % 4;
+                            if constexpr (ND == 2) y[h][k] = fin.half(t[2 * h][r], t[2 * h + 1][r]);
+                            else if constexpr (ND == 3) y[h][k] = fin.half(t[3 * h][r], t[3 * h + 1][r], t[3 * h + 2][r]);
+                            else y[h][k] = fin.half(t[4 * h][r], t[4 * h + 1][r], t[4 * h + 2][r], t[4 * h + 3][r]);
+                        }
+                    fin.store(dst + mine * out_stride, ends[mine], y[0], y[1]);
                 }
                 __builtin_amdgcn_sched_barrier(0);           // one output at a time: its temporaries are few
             }
@@ -310,37 +322,38 @@ struct Place {
     u32 part, run, row;
 };
 __device__ __forceinline__ Place place_of(u32 parts, u32 runs) {
-    const u32 side = min(parts, 8u);  // (parts is a power of two, below eight for packed residues at N = 2^10)
+    const u32 side = min(parts, 8u);  // (parts is a power of two)
     u32 b = blockIdx.x / side;
     const u32 run = b % runs;
     b /= runs;
     return Place{b % (parts / side) * side + blockIdx.x % side, run, b / (parts / side)};
 }
 
-template <typename V>
+template <typename V, int RT>
 __global__ void __launch_bounds__(THREADS, 2) i8_whole_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
-    __shared__ Ends lds[WHOLE_RUN * 32];
-    const Place at = place_of(a.N / whole_slots<V>(), a.runs);
+    __shared__ Ends lds[WHOLE_RUN * 16 * RT];
+    const Place at = place_of(a.N / (blockDim.x * 4 / sizeof(V)), a.runs);
     const u32 begin = at.run * a.run, end = min(begin + a.run, a.n_groups);
     const LimbConst& c = lt.c[at.row >> 1];
     const I8Limb& l = lc.c[at.row >> 1];
-    if constexpr (sizeof(V) == 4) whole_body<V, 4>(a, c, l, at.part, at.row, begin, end, lds);
-    else if (l.nd == 4) whole_body<V, 4>(a, c, l, at.part, at.row, begin, end, lds);
-    else if (l.nd == 3) whole_body<V, 3>(a, c, l, at.part, at.row, begin, end, lds);
-    else whole_body<V, 2>(a, c, l, at.part, at.row, begin, end, lds);
+    if constexpr (sizeof(V) == 4) whole_body<V, RT, 4>(a, c, l, at.part, at.row, begin, end, lds);
+    else if (l.nd == 4) whole_body<V, RT, 4>(a, c, l, at.part, at.row, begin, end, lds);
+    else if (l.nd == 3) whole_body<V, RT, 3>(a, c, l, at.part, at.row, begin, end, lds);
+    else whole_body<V, RT, 2>(a, c, l, at.part, at.row, begin, end, lds);
 }
 
 // ---------------------------------------------------------------------------------------------
-// Second form: 2 OT tiles of 32 outputs.  A workgroup takes 64 units of eight bytes and 64 terms at a time: each wavefront loads 16 of the
-// terms, 16 bytes of a row per lane, transposes them and writes the operands to the LDS; then it multiplies the digits of its half by
-// its OT tiles.  Unit 2 l + k of the 64 is column l of column tile k, so that a lane ends up with two neighbouring units.
+// Second form: two tiles of 32 outputs.  A workgroup takes 64 units of eight bytes and 64 terms at a time: each wavefront loads 16 of the
+// terms, 16 bytes of a row per lane, transposes them and writes the operands to the LDS; then it multiplies the digits of one half by
+// one of the tiles.  Unit 2 l + k of the 64 is column l of column tile k, so that a lane ends up with two neighbouring units.
 
 // Operands of 64 terms: [block of 32 terms][digit][column tile][lane], twice (one is filled while the other is multiplied).
 constexpr u32 OPERAND_PIECES = 2 * 8 * 2 * 64;
+constexpr u32 LIST_STEPS = 32;  // steps whose list is in the LDS
 
-template <typename V, int OT, int ND>
+template <typename V, int ND>
 __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb_const, const I8Group& g, u32 part, u32 row, Ends* ends,
-                                           v4i* lds) {
+                                           v4i* lds, u32* ct_list) {
     const u32 lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32, col = lane % 32;
     constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit
     const u32 comp = row & 1, limb = row >> 1;
@@ -348,56 +361,42 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
     const size_t at = ((size_t)comp * a.limbs + limb) * a.N + slot;
     const u32 ct_stride = 2 * a.limbs * a.N * sizeof(V);     // bytes
     const char* x_base = reinterpret_cast<const char*>(a.ct_in + at);
-    const u32 blocks = (g.n_terms + 31) / 32;
-    const u32 upper = wave & 1, tile0 = wave / 2 * OT;       // what this wavefront multiplies
+    const u32 upper = wave & 1, tile = wave / 2;           // what this wavefront multiplies
     const u32 load_block = wave / 2, load_half = wave & 1;   // what it loads: 16 terms of one of the two blocks, eight per lane
-    const u32* list = a.lists + (size_t)g.list * 32 + load_half * 16 + half * 8;
-    const v4i* table = a.table + ((size_t)g.table + tile0) * 64 + lane;
-    if (threadIdx.x < g.count) ends[threadIdx.x] = ends_of(a, c, row, g.out0 + threadIdx.x);
+    const v4i* table = a.table + (size_t)g.table * 32 + tile * 64 + lane;
+    if (threadIdx.x < g.count) ends[threadIdx.x] = ends_of(a, row, g.out0 + threadIdx.x, c.q);
 
-    v16i sums[OT][2][ND];
+    v16i sums[2][ND];
 #pragma unroll
-    for (int o = 0; o < OT; o++)
+    for (int k = 0; k < 2; k++)
 #pragma unroll
-        for (int k = 0; k < 2; k++)
+        for (int d = 0; d < ND; d++)
 #pragma unroll
-            for (int d = 0; d < ND; d++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) sums[o][k][d][i] = 0;
+            for (int i = 0; i < 16; i++) sums[k][d][i] = 0;
 
-    // Step s multiplies blocks 2 s and 2 s + 1 while the residues of step s + 1 become its operands; those of AHEAD steps more are
-    // on their way (one where two workgroups share a compute unit); past the end the last block's are requested again.
-    constexpr int AHEAD = OT == 1 ? 1 : 2;
-    u32 idx[8];
-    u32x4 x[AHEAD][8];
-    v4i w[2][OT];
-    auto request_idx = [&](u32 s) {
-        const u32* p = list + (size_t)min(2 * s + load_block, blocks - 1) * 32;
+    // Step s multiplies blocks 2 s and 2 s + 1 while the residues of step s + 1 become its operands; those of steps s + 2 and s + 3 are on
+    // their way; past the end the last step's are requested again.  Loads complete in order: what is waited for sooner is requested first, and
+    // the list lies in the LDS, LIST_STEPS steps of it at a time.
+    u32 steps, step0;  // of this part of the list
+    u32x4 x[2][8];
+    v4i w[2][2];       // [step's parity][block]
+    auto request_x = [&](u32 s, u32x4 (&to)[8]) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(ct_list + min(s, steps - 1) * 64 + load_block * 32 + load_half * 16 + half * 8);
+        const u32x4 i0 = p[0], i1 = p[1];
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * j);
-#pragma unroll
-            for (int k = 0; k < 4; k++) idx[4 * j + k] = v[k];
-        }
+        for (int k = 0; k < 8; k++) to[k] = *reinterpret_cast<const u32x4*>(x_base + (u64)(k < 4 ? i0[k] : i1[k - 4]) * ct_stride);
     };
-    auto request_x = [&](u32x4 (&to)[8]) {
+    auto request_w = [&](u32 s, v4i (&to)[2]) {
 #pragma unroll
-        for (int k = 0; k < 8; k++) to[k] = *reinterpret_cast<const u32x4*>(x_base + (u64)idx[k] * ct_stride);
-    };
-    auto request_w = [&](u32 block, v4i (&to)[OT]) {
-#pragma unroll
-        for (int o = 0; o < OT; o++) to[o] = table[((size_t)min(block, blocks - 1) * (2 * OT) + o) * 64];
+        for (int b = 0; b < 2; b++) to[b] = table[((size_t)(step0 + min(s, steps - 1)) * 2 + b) * (2 * 64)];
     };
     // one half of the digits of column tile k: eight terms
     auto write_operand = [&](v4i* to, const u32x4 (&from)[8], int k, int h) {
         u32 t[2][ND];
 #pragma unroll
         for (int j = 0; j < 2; j++) {
-            auto bytes = [&](int i) -> u32 {  // the second half's start at byte ND
-                const u32 lo = from[i][2 * k], hi = from[i][2 * k + 1];
-                return h == 0 ? lo : ND == 4 ? hi : __builtin_amdgcn_alignbyte(hi, lo, ND);
-            };
-            transpose4<ND>(bytes(4 * j), bytes(4 * j + 1), bytes(4 * j + 2), bytes(4 * j + 3), t[j]);
+            transpose4<ND>(half_bytes<ND>(from[4 * j], k, h), half_bytes<ND>(from[4 * j + 1], k, h), half_bytes<ND>(from[4 * j + 2], k, h),
+                           half_bytes<ND>(from[4 * j + 3], k, h), t[j]);
         }
 #pragma unroll
         for (int d = 0; d < ND; d++) {
@@ -407,114 +406,120 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
     };
     auto multiply = [&](auto of_parity, u32 s) {
         constexpr int P = decltype(of_parity)::value;
-        const v4i* from = lds + P * OPERAND_PIECES + lane;
+        const v4i* from = lds + P * OPERAND_PIECES + upper * (ND * 2 * 64) + lane;
         v4i* to = lds + (P ^ 1) * OPERAND_PIECES;
         lds_barrier();  // the operands of this step are in place, and nobody reads the others any more
+        v4i in[ND];     // the next ND operands: of digit d, block q / 2 and column tile q % 2
 #pragma unroll
-        for (int q = 0; q < 4; q++) {  // block q / 2, column tile q % 2; a fourth of the next step's operands
-            if (q < 2 || 2 * s + 1 < blocks) {
+        for (int d = 0; d < ND; d++) in[d] = from[(d * 2) * 64];
 #pragma unroll
-                for (int d = 0; d < ND; d++) {
-                    const v4i in = from[((q / 2 * 8 + upper * ND + d) * 2 + q % 2) * 64];
+        for (int q = 0; q < 4; q++) {  // a fourth of the products, and of the next step's operands
 #pragma unroll
-                    for (int o = 0; o < OT; o++)
-                        sums[o][q % 2][d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q / 2][o], in, sums[o][q % 2][d], 0, 0, 0);
-                }
+            for (int d = 0; d < ND; d++) {
+                sums[q % 2][d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[P][q / 2], in[d], sums[q % 2][d], 0, 0, 0);
+                if (q < 3) in[d] = from[(((q + 1) / 2 * 8 + d) * 2 + (q + 1) % 2) * 64];
             }
-            if (q % 2) request_w(2 * s + 2 + q / 2, w[q / 2]);
-            write_operand(to, x[(P ^ 1) % AHEAD], q % 2, q / 2);
+            write_operand(to, x[P ^ 1], q % 2, q / 2);
+#pragma unroll
+            for (int d = 0; d < ND; d++) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product,
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an operand of the next fourth,
+                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);  // and a share of the arithmetic behind them
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
-        request_x(x[(P ^ 1) % AHEAD]);
-        request_idx(s + AHEAD + 2);
+        request_w(s + 2, w[P]);
+        request_x(s + 3, x[P ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
     };
-    if (blocks) {
-        const u32 steps = (blocks + 1) / 2;
+    const u32 all_steps = (g.n_terms + 63) / 64;
+    for (step0 = 0; step0 < all_steps; step0 += LIST_STEPS) {
+        steps = min(all_steps - step0, LIST_STEPS);
+        for (u32 i = threadIdx.x; i < steps * 64; i += THREADS) ct_list[i] = a.lists[(size_t)g.list * 32 + step0 * 64 + i];
+        lds_barrier();
         request_w(0, w[0]);
         request_w(1, w[1]);
-        request_idx(0);
-        request_x(x[0]);
-        request_idx(1);
-        if constexpr (AHEAD == 2) {
-            request_x(x[1]);
-            request_idx(2);
-        }
+        request_x(0, x[0]);
+        request_x(1, x[1]);
 #pragma unroll
         for (int q = 0; q < 4; q++) write_operand(lds, x[0], q % 2, q / 2);
-        request_x(x[0]);
-        request_idx(AHEAD + 1);
+        request_x(2, x[0]);
         u32 s = 0;
         for (; s + 1 < steps; s += 2) {
             multiply(std::integral_constant<int, 0>{}, s);
             multiply(std::integral_constant<int, 1>{}, s + 1);
         }
         if (s < steps) multiply(std::integral_constant<int, 0>{}, s);
-        lds_barrier();  // (the operands are not read any more)
+        lds_barrier();  // (the operands and the list are not read any more)
     }
 
-    const End<V, 2> fin = end_of<V, 2>(a, c, limb_const, row, slot);
+    const End<V> fin = end_of(a, c, limb_const, row, slot);
     const size_t out_stride = (size_t)2 * a.limbs * a.N;
     V* const dst = a.out + g.out0 * out_stride + at;
-    auto sum = [&](int o, int k, int r) {
-        const v16i (&t)[ND] = sums[o][k];
-        return fin.template half<ND>(t[0][r], t[1][r], ND > 2 ? t[ND > 2 ? 2 : 0][r] : 0, ND > 3 ? t[ND > 3 ? 3 : 0][r] : 0);
+    auto sum = [&](int k, int r) {
+        const v16i (&t)[ND] = sums[k];
+        if constexpr (ND == 2) return fin.half(t[0][r], t[1][r]);
+        else if constexpr (ND == 3) return fin.half(t[0][r], t[1][r], t[2][r]);
+        else return fin.half(t[0][r], t[1][r], t[2][r], t[3][r]);
     };
-    // Of every tile the wavefront of the lower digits finishes the first eight of a lane's outputs, the other one the last eight: they exchange the
-    // others' sums.
+    // The wavefront of the lower digits finishes the first eight of a lane's outputs, the other one the last eight: they exchange the others' sums.
     auto finish = [&](auto of_upper) {
         constexpr bool UPPER = decltype(of_upper)::value;
         constexpr int KEEP = UPPER ? 8 : 0, SEND = 8 - KEEP;
-        u64* exchange = reinterpret_cast<u64*>(lds) + lane;  // [tile parity][wavefront][output][column tile][lane]
+        u64* exchange = reinterpret_cast<u64*>(lds) + lane;  // [wavefront][output][column tile][lane]
 #pragma unroll
-        for (int o = 0; o < OT; o++) {
-            u64* buf = exchange + (o & 1) * (WAVES * 16 * 64);
+        for (int i = 0; i < 16; i++) exchange[(wave * 16 + i) * 64] = sum(i % 2, SEND + i / 2);
+        lds_barrier();  // (also for the ends)
 #pragma unroll
-            for (int i = 0; i < 16; i++) buf[(wave * 16 + i) * 64] = sum(o, i % 2, SEND + i / 2);
-            lds_barrier();  // (also for the ends)
+        for (int i = 0; i < 8; i++) {
+            const u32 r = KEEP + i, mine = 32 * tile + 8 * (r / 4) + 4 * half + r % 4;
+            if (mine < g.count) {
+                u64 own_sum[2], other[2];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const u32 r = KEEP + i, mine = 32 * (tile0 + o) + 8 * (r / 4) + 4 * half + r % 4;
-                if (mine < g.count) {
-                    const Ends e = ends[mine];
-                    V* const p = dst + mine * out_stride;
-                    u64 own_sum[2], other[2];
-#pragma unroll
-                    for (int k = 0; k < 2; k++) own_sum[k] = sum(o, k, KEEP + i), other[k] = buf[((wave ^ 1) * 16 + 2 * i + k) * 64];
-                    fin.store(p, e, UPPER ? other : own_sum, UPPER ? own_sum : other);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                for (int k = 0; k < 2; k++) own_sum[k] = sum(k, KEEP + i), other[k] = exchange[((wave ^ 1) * 16 + 2 * i + k) * 64];
+                fin.store(dst + mine * out_stride, ends[mine], UPPER ? other : own_sum, UPPER ? own_sum : other);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     if (upper) finish(std::true_type{});
     else finish(std::false_type{});
 }
 
-template <typename V, int OT>
-__global__ void __launch_bounds__(THREADS, OT == 1 ? 2 : 1) i8_split_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
-    __shared__ Ends ends[64 * OT];
+template <typename V>
+__global__ void __launch_bounds__(THREADS, 2) i8_split_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
+    __shared__ Ends ends[64];
     __shared__ v4i lds[2 * OPERAND_PIECES];
+    __shared__ __align__(16) u32 ct_list[LIST_STEPS * 64];
     const Place at = place_of(a.N / split_slots<V>(), a.runs);
     const I8Group g = load_group(a.groups + a.first + at.run);
     const LimbConst& c = lt.c[at.row >> 1];
     const I8Limb& l = lc.c[at.row >> 1];
-    if constexpr (sizeof(V) == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, lds);
-    else if (l.nd == 4) split_body<V, OT, 4>(a, c, l, g, at.part, at.row, ends, lds);
-    else if (l.nd == 3) split_body<V, OT, 3>(a, c, l, g, at.part, at.row, ends, lds);
-    else split_body<V, OT, 2>(a, c, l, g, at.part, at.row, ends, lds);
+    if constexpr (sizeof(V) == 4) split_body<V, 4>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    else if (l.nd == 4) split_body<V, 4>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    else if (l.nd == 3) split_body<V, 3>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    else split_body<V, 2>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
 }
 
 template <typename V>
 u32 class_count(const he_i8_layer* l, u32 cls) { return l->class_begin[cls + 1] - l->class_begin[cls]; }
 
-// workgroups of a class; *run: the groups that each of them takes
+// How a class is launched: the groups that a workgroup takes, its threads, and the workgroups.
+struct Launch {
+    u32 run, threads;
+    u64 blocks;
+};
 template <typename V>
-u64 class_blocks(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls, u32* run) {
-    const u64 rows = 2 * limbs, parts = ctx->N / (cls == 0 ? whole_slots<V>() : split_slots<V>()), count = class_count<V>(l, cls);
-    *run = cls == 0 ? WHOLE_RUN : 1;
-    while (*run > 1 && (count + *run - 1) / *run * parts * rows < MIN_WORKGROUPS) *run /= 2;
-    return (count + *run - 1) / *run * parts * rows;
+Launch class_launch(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls) {
+    const u64 rows = 2 * limbs, count = class_count<V>(l, cls);
+    if (cls >= 2) return Launch{1, THREADS, count * (ctx->N / split_slots<V>()) * rows};
+    // The first form's wavefronts are independent: a small launch has one per workgroup, to reach every compute unit.
+    Launch k{WHOLE_RUN, THREADS, 0};
+    auto blocks = [&] { return (count + k.run - 1) / k.run * (ctx->N / (k.threads * 4 / sizeof(V))) * rows; };
+    while (k.run > 1 && blocks() < MIN_WORKGROUPS) k.run /= 2;
+    if (blocks() < SMALL_LAUNCH) k.threads = 64;
+    k.blocks = blocks();
+    return k;
 }
 
 template <typename V, int CLS>
@@ -522,10 +527,12 @@ int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) 
     a.first = l->class_begin[CLS];
     a.n_groups = class_count<V>(l, CLS);
     if (a.n_groups == 0) return HE_OK;
-    const dim3 grid((u32)class_blocks<V>(ctx, l, a.limbs, CLS, &a.run)), block(THREADS);
+    const Launch k = class_launch<V>(ctx, l, a.limbs, CLS);
+    const dim3 grid((u32)k.blocks), block(k.threads);
+    a.run = k.run;
     a.runs = (a.n_groups + a.run - 1) / a.run;
-    if constexpr (CLS == 0) hipLaunchKernelGGL(i8_whole_kernel<V>, grid, block, 0, s, ctx->limbs, l->limbs, a);
-    else hipLaunchKernelGGL((i8_split_kernel<V, CLS>), grid, block, 0, s, ctx->limbs, l->limbs, a);
+    if constexpr (CLS < 2) hipLaunchKernelGGL((i8_whole_kernel<V, CLS + 1>), grid, block, 0, s, ctx->limbs, l->limbs, a);
+    else hipLaunchKernelGGL(i8_split_kernel<V>, grid, block, 0, s, ctx->limbs, l->limbs, a);
     HE_HIP(hipGetLastError());
     return HE_OK;
 }
@@ -555,10 +562,31 @@ struct Rows {
 
 // every launch of a call must fit a grid
 int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed) {
-    u32 run;
     for (u32 cls = 0; cls < I8_CLASSES; cls++)
-        if ((packed ? class_blocks<u32>(ctx, l, limbs, cls, &run) : class_blocks<u64>(ctx, l, limbs, cls, &run)) > 0x7FFFFFFFull) return HE_ERR_RANGE;
+        if ((packed ? class_launch<u32>(ctx, l, limbs, cls) : class_launch<u64>(ctx, l, limbs, cls)).blocks > 0x7FFFFFFFull) return HE_ERR_RANGE;
     return HE_OK;
+}
+
+void fill_i8_limb(I8Limb& c, u64 q) {
+    u32 bits = 0;
+    while (q >> bits) bits++;
+    c.q = q;
+    c.two_q = 2 * q;
+    c.nd = std::max<u32>(2, ((bits + 7) / 8 + 1) / 2);
+    c.exact = q >= 1ull << 60;
+    c.bits_shift = bits - 8;
+    c.mult = (u32)(((u128)1 << (16 + c.bits_shift)) / q);
+}
+
+I8Channel i8_channel(const I8Limb& c, u64 s, int64_t weight_sum, bool packed) {
+    const u64 q = c.q, shift = (u64)(((u128)1 << (8 * c.nd)) % q), offset = (1ull << I8_OFFSET_BITS) % q;
+    u64 flipped = 0;  // what the digits' top bits stand for: all of them, or the four of packed storage
+    for (u32 d = 0; d < (packed ? 4 : 2 * c.nd); d++) flipped |= 0x80ull << (8 * d);
+    const u64 sum = (u64)(((__int128)weight_sum % (__int128)q + q) % q);
+    const u64 offsets = packed ? offset : (u64)(((u128)offset + mul_mod_host(offset, shift, q)) % q);
+    const u64 s1 = mul_mod_host(s, shift, q);
+    return I8Channel{s, (u64)(((u128)s << 64) / q), s1, (u64)(((u128)s1 << 64) / q),
+                     mul_mod_host(s, (mul_mod_host(flipped % q, sum, q) + q - offsets) % q, q)};
 }
 
 // The host's part of a layer: groups, lists, table and constants (throws std::bad_alloc).
@@ -566,21 +594,21 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
                     he_i8_layer* l, I8Host& h) {
     const Rows rows{off, term_ct, term_pt};
     const u32 n_out = l->n_out;
-    // Runs of outputs that read the same inputs in the same order, cut into groups of up to 128 with the same number of tiles.
+    // Runs of outputs that read the same inputs in the same order, cut into groups of up to 64 with the same number of tiles.
     std::vector<I8Group> classes[I8_CLASSES];
     std::unordered_multimap<u64, I8Group> known;  // groups by a hash of their weights, to share tables
     for (u32 o = 0; o < n_out;) {
         u32 end = o + 1;
         while (end < n_out && rows.same_inputs(o, end)) end++;
-        const u32 terms = rows.terms(o), blocks = (terms + 31) / 32;
-        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + 3) / 4, each = (tiles + cuts - 1) / cuts * 32;
+        const u32 terms = rows.terms(o), pad = end - o > 32 ? 64 : 32, blocks = (terms + pad - 1) / pad * (pad / 32);
+        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + 1) / 2, each = (tiles + cuts - 1) / cuts * 32;
         const u32 list = (u32)(h.lists.size() / 32);
         for (u32 t = 0; t < blocks * 32; t++) h.lists.push_back(term_ct[off[o] + std::min(t, terms - 1)]);
         for (u32 count; o < end; o += count) {
             count = std::min(each, end - o);
             I8Group g{o, count, terms, list, 0, {0, 0, 0}};
             // (outputs without terms go to the second form, whose loop over the blocks may be empty)
-            const u32 cls = count > 64 ? 2 : count > 32 || terms == 0 ? 1 : 0, per = 1u << cls;
+            const u32 cls = count > 32 || terms == 0 ? 2 : count > 16 ? 1 : 0;
             const size_t n = (size_t)g.count * terms;  // the plaintexts of a group's outputs follow one another
             u64 hash = 0xCBF29CE484222325ull ^ n;
             for (size_t i = 0; i < n; i++) hash = (hash ^ term_pt[off[o] + i]) * 0x100000001B3ull;
@@ -593,13 +621,20 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
                 found = true;
             }
             if (!found) {
-                // [block][tile][lane][16]: row lane % 32 of the tile, terms 16 * (lane / 32) .. of the block
-                g.table = (u32)(h.table.size() / 1024);
-                h.table.resize(h.table.size() + (size_t)blocks * per * 1024, 0);
-                int8_t* t0 = h.table.data() + (size_t)g.table * 1024;
-                for (u32 r = 0; r < g.count; r++)
-                    for (u32 t = 0; t < terms; t++)
-                        t0[(((size_t)t / 32 * per + r / 32) * 64 + t % 32 / 16 * 32 + r % 32) * 16 + t % 16] = weights[term_pt[off[o + r] + t]];
+                // First form: [block][tile of 16 rows][lane][8], lane's row lane % 16 (output 4 (row % 4) + row / 4 of the tile), terms 8 (lane / 16) .. of the
+                // block.  Second form: [block][tile of 32 rows][lane][16], row lane % 32, terms 16 (lane / 32) ..
+                const u32 units = cls < 2 ? cls + 1 : 4;  // of 512 bytes, per block
+                g.table = (u32)(h.table.size() / 512);
+                h.table.resize(h.table.size() + (size_t)blocks * units * 512, 0);
+                int8_t* t0 = h.table.data() + (size_t)g.table * 512;
+                for (u32 r = 0; r < g.count; r++) {
+                    const u32 row = r % 4 * 4 + r % 16 / 4;
+                    for (u32 t = 0; t < terms; t++) {
+                        const size_t at = cls < 2 ? (((size_t)t / 32 * units + r / 16) * 64 + t % 32 / 8 * 16 + row) * 8 + t % 8
+                                                  : (((size_t)t / 32 * (units / 2) + r / 32) * 64 + t % 32 / 16 * 32 + r % 32) * 16 + t % 16;
+                        t0[at] = weights[term_pt[off[o + r] + t]];
+                    }
+                }
                 known.emplace(hash, g);
             }
             classes[cls].push_back(g);
@@ -617,21 +652,11 @@ void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const
     h.channels.resize((size_t)ctx->L * n_out);
     h.channels32.resize((size_t)ctx->L * n_out);
     for (u32 i = 0; i < ctx->L; i++) {
-        const u64 q = ctx->q[i];
-        u32 bits = 0;
-        while (q >> bits) bits++;
-        const u32 nd = std::max<u32>(2, ((bits + 7) / 8 + 1) / 2);
-        const u64 shift = (u64)(((u128)1 << (8 * nd)) % q), offset = (1ull << OFFSET_BITS) % q;
-        l->limbs.c[i] = I8Limb{nd, q < (1ull << 61), shift, (u64)(((u128)shift << 64) / q)};
-        u64 flipped = 0;  // what the digits' top bits stand for, all 2 nd of them
-        for (u32 d = 0; d < 2 * nd; d++) flipped |= 0x80ull << (8 * d);
-        const u64 both = (u64)(((u128)offset + mul_mod_host(offset, shift, q)) % q);
+        fill_i8_limb(l->limbs.c[i], ctx->q[i]);
         for (u32 o = 0; o < n_out; o++) {
-            const u64 s = scale ? scale[(size_t)o * ctx->L + i] : 1, s_shoup = (u64)(((u128)s << 64) / q);
-            const u64 sum = (u64)(((__int128)weight_sum[o] % (__int128)q + q) % q);
-            const size_t k = (size_t)i * n_out + o;
-            h.channels[k] = I8Channel{s, s_shoup, mul_mod_host(s, (mul_mod_host(flipped % q, sum, q) + q - both) % q, q)};
-            h.channels32[k] = I8Channel{s, s_shoup, mul_mod_host(s, (mul_mod_host(0x80808080u % q, sum, q) + q - offset) % q, q)};
+            const u64 s = scale ? scale[(size_t)o * ctx->L + i] : 1;
+            h.channels[(size_t)i * n_out + o] = i8_channel(l->limbs.c[i], s, weight_sum[o], false);
+            h.channels32[(size_t)i * n_out + o] = i8_channel(l->limbs.c[i], s, weight_sum[o], true);
         }
     }
 }

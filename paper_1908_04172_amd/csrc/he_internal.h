@@ -151,25 +151,15 @@ struct he_plan {
 };
 
 // ---- int8 layers (he_i8.hip)
-constexpr u32 I8_CLASSES = 3;          // groups of up to 32, 64 and 128 outputs
+constexpr u32 I8_CLASSES = 3;          // groups of up to 16, 32 and 64 outputs
 constexpr u32 I8_MAX_TERMS = 131071;   // of an output: sums of so many products of at most 2^14 stay below 2^31
 // Outputs that read the same ciphertexts in the same order.
 struct I8Group {
     u32 out0, count;
     u32 n_terms;   // of each output
     u32 list;      // where the ciphertexts of the terms start in he_i8_layer::lists_dev, in blocks of 32 terms
-    u32 table;     // where the weights start in he_i8_layer::table_dev, in tiles of 1024 bytes
+    u32 table;     // where the weights start in he_i8_layer::table_dev, in units of 512 bytes
     u32 pad[3];
-};
-// An output's scale modulo a limb, its Shoup companion, and what is left to add (he_i8.hip).
-struct I8Channel {
-    u64 s, s_shoup, addend;
-};
-// Per limb: how many digits of a residue one half of them has (2, 3 or 4), and 256^nd mod q with its Shoup companion.
-struct I8Limb {
-    u32 nd;
-    u32 cheap;  // 1: q < 2^61, the cheap quotient estimate serves
-    u64 shift, shift_shoup;
 };
 struct I8Limbs {
     I8Limb c[HE_MAX_LIMBS];
@@ -285,6 +275,8 @@ int launch_rescale32(he_ctx* ctx, u32 limbs, const u32* in, u32* out, u32 n, hip
 int launch_encode_vector(he_ctx* ctx, u32 limbs, const double* slots, u32 n, double scale, u64* out, hipStream_t s);
 int launch_decode_vector(he_ctx* ctx, u32 limbs, const u64* coef, u32 n, double scale, double* slots, hipStream_t s);
 // int8 layers (he_i8.hip); scale: host [n_out][L] residues or null
+void fill_i8_limb(I8Limb& c, u64 q);
+I8Channel i8_channel(const I8Limb& c, u64 s, int64_t weight_sum, bool packed);
 void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const u32* term_pt, const int8_t* weights, const u64* scale,
                     he_i8_layer* l, I8Host& h);
 int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed);
