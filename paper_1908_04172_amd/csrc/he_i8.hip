@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <type_traits>
 #include <unordered_map>
+#include <unordered_set>
 
 #include "he_internal.h"
 
@@ -32,7 +33,7 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
-constexpr u32 THREADS = 256, WAVES = THREADS / 64;
+constexpr u32 THREADS = 256;
 constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most
 constexpr u64 MIN_WORKGROUPS = 2048; // ... while the launch keeps at least this many workgroups
 constexpr u64 SMALL_LAUNCH = 512;    // workgroups
@@ -110,7 +111,8 @@ __device__ __forceinline__ Ends ends_of(const I8Args<V>& a, u32 row, u32 output,
 }
 
 // What the ends of all outputs of a row have in common, for two neighbouring units of eight bytes per lane.
-template <typename V>
+// STREAM: the stores go past the caches (stores_stream); by a branch per output both kinds would be the plain one.
+template <typename V, bool STREAM>
 struct End {
     static constexpr int SLOTS = 16 / sizeof(V);
     I8Limb c;
@@ -146,13 +148,14 @@ struct End {
 #pragma unroll
             for (int k = 0; k < SLOTS; k++) v[k] = (V)add_mod(v[k], old[k], c.q);
         }
-        *reinterpret_cast<piece*>(p) = v;
+        if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<piece*>(p));
+        else *reinterpret_cast<piece*>(p) = v;
     }
 };
 
-template <typename V>
-__device__ __forceinline__ End<V> end_of(const I8Args<V>& a, const LimbConst& lc, const I8Limb& limb, u32 row, u32 slot) {
-    End<V> e;
+template <typename V, bool STREAM>
+__device__ __forceinline__ End<V, STREAM> end_of(const I8Args<V>& a, const LimbConst& lc, const I8Limb& limb, u32 row, u32 slot) {
+    End<V, STREAM> e;
     e.c = limb;
     e.has_token = a.token != nullptr;
     e.accumulate = a.accumulate;
@@ -203,7 +206,7 @@ __device__ __forceinline__ void step(Cursor& c, const I8Args<V>& a, u32 end) {  
     else if (c.group + 1 < end) c = enter(a, c.group + 1);
 }
 
-template <typename V, int RT, int ND>
+template <typename V, int RT, bool STREAM, int ND>
 __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& lc, const I8Limb& limb_const, u32 part, u32 row, u32 begin, u32 end, Ends* lds) {
     const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64, quarter = lane / 16, col = lane % 16;
     constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit
@@ -218,7 +221,7 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
         const I8Group& g = a.groups[a.first + begin + i / (16 * RT)];
         if (i % (16 * RT) < g.count) lds[i] = ends_of(a, row, g.out0 + i % (16 * RT), lc.q);
     }
-    const End<V> fin = end_of(a, lc, limb_const, row, slot);
+    const End<V, STREAM> fin = end_of<V, STREAM>(a, lc, limb_const, row, slot);
     __syncthreads();
 
     Cursor cur = enter(a, begin), nxt = cur;
@@ -329,17 +332,17 @@ __device__ __forceinline__ Place place_of(u32 parts, u32 runs) {
     return Place{b % (parts / side) * side + blockIdx.x % side, run, b / (parts / side)};
 }
 
-template <typename V, int RT>
+template <typename V, int RT, bool STREAM>
 __global__ void __launch_bounds__(THREADS, 2) i8_whole_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
     __shared__ Ends lds[WHOLE_RUN * 16 * RT];
     const Place at = place_of(a.N / (blockDim.x * 4 / sizeof(V)), a.runs);
     const u32 begin = at.run * a.run, end = min(begin + a.run, a.n_groups);
     const LimbConst& c = lt.c[at.row >> 1];
     const I8Limb& l = lc.c[at.row >> 1];
-    if constexpr (sizeof(V) == 4) whole_body<V, RT, 4>(a, c, l, at.part, at.row, begin, end, lds);
-    else if (l.nd == 4) whole_body<V, RT, 4>(a, c, l, at.part, at.row, begin, end, lds);
-    else if (l.nd == 3) whole_body<V, RT, 3>(a, c, l, at.part, at.row, begin, end, lds);
-    else whole_body<V, RT, 2>(a, c, l, at.part, at.row, begin, end, lds);
+    if constexpr (sizeof(V) == 4) whole_body<V, RT, STREAM, 4>(a, c, l, at.part, at.row, begin, end, lds);
+    else if (l.nd == 4) whole_body<V, RT, STREAM, 4>(a, c, l, at.part, at.row, begin, end, lds);
+    else if (l.nd == 3) whole_body<V, RT, STREAM, 3>(a, c, l, at.part, at.row, begin, end, lds);
+    else whole_body<V, RT, STREAM, 2>(a, c, l, at.part, at.row, begin, end, lds);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -351,7 +354,7 @@ __global__ void __launch_bounds__(THREADS, 2) i8_whole_kernel(LimbTable lt, I8Li
 constexpr u32 OPERAND_PIECES = 2 * 8 * 2 * 64;
 constexpr u32 LIST_STEPS = 32;  // steps whose list is in the LDS
 
-template <typename V, int ND>
+template <typename V, bool STREAM, int ND>
 __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& c, const I8Limb& limb_const, const I8Group& g, u32 part, u32 row, Ends* ends,
                                            v4i* lds, u32* ct_list) {
     const u32 lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32, col = lane % 32;
@@ -453,7 +456,7 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
         lds_barrier();  // (the operands and the list are not read any more)
     }
 
-    const End<V> fin = end_of(a, c, limb_const, row, slot);
+    const End<V, STREAM> fin = end_of<V, STREAM>(a, c, limb_const, row, slot);
     const size_t out_stride = (size_t)2 * a.limbs * a.N;
     V* const dst = a.out + g.out0 * out_stride + at;
     auto sum = [&](int k, int r) {
@@ -486,7 +489,7 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
     else finish(std::false_type{});
 }
 
-template <typename V>
+template <typename V, bool STREAM>
 __global__ void __launch_bounds__(THREADS, 2) i8_split_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
     __shared__ Ends ends[64];
     __shared__ v4i lds[2 * OPERAND_PIECES];
@@ -495,10 +498,10 @@ __global__ void __launch_bounds__(THREADS, 2) i8_split_kernel(LimbTable lt, I8Li
     const I8Group g = load_group(a.groups + a.first + at.run);
     const LimbConst& c = lt.c[at.row >> 1];
     const I8Limb& l = lc.c[at.row >> 1];
-    if constexpr (sizeof(V) == 4) split_body<V, 4>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
-    else if (l.nd == 4) split_body<V, 4>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
-    else if (l.nd == 3) split_body<V, 3>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
-    else split_body<V, 2>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    if constexpr (sizeof(V) == 4) split_body<V, STREAM, 4>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    else if (l.nd == 4) split_body<V, STREAM, 4>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    else if (l.nd == 3) split_body<V, STREAM, 3>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
+    else split_body<V, STREAM, 2>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
 }
 
 template <typename V>
@@ -522,7 +525,7 @@ Launch class_launch(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls)
     return k;
 }
 
-template <typename V, int CLS>
+template <typename V, bool STREAM, int CLS>
 int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) {
     a.first = l->class_begin[CLS];
     a.n_groups = class_count<V>(l, CLS);
@@ -531,8 +534,8 @@ int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) 
     const dim3 grid((u32)k.blocks), block(k.threads);
     a.run = k.run;
     a.runs = (a.n_groups + a.run - 1) / a.run;
-    if constexpr (CLS < 2) hipLaunchKernelGGL((i8_whole_kernel<V, CLS + 1>), grid, block, 0, s, ctx->limbs, l->limbs, a);
-    else hipLaunchKernelGGL(i8_split_kernel<V>, grid, block, 0, s, ctx->limbs, l->limbs, a);
+    if constexpr (CLS < 2) hipLaunchKernelGGL((i8_whole_kernel<V, CLS + 1, STREAM>), grid, block, 0, s, ctx->limbs, l->limbs, a);
+    else hipLaunchKernelGGL((i8_split_kernel<V, STREAM>), grid, block, 0, s, ctx->limbs, l->limbs, a);
     HE_HIP(hipGetLastError());
     return HE_OK;
 }
@@ -541,10 +544,13 @@ template <typename V>
 int launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const V* ct_in, const V* token, const u64* bias, V* out, u32 accumulate, hipStream_t s) {
     const I8Args<V> a{l->groups_dev, l->lists_dev, reinterpret_cast<const v4i*>(l->table_dev), sizeof(V) == 8 ? l->channels_dev : l->channels32_dev,
                       ct_in, token, bias, out, limbs, ctx->N, l->n_out, 0, 0, 0, 0, accumulate};
-    int rc;
-    if ((rc = launch_class<V, 0>(ctx, a, l, s)) != HE_OK) return rc;
-    if ((rc = launch_class<V, 1>(ctx, a, l, s)) != HE_OK) return rc;
-    return launch_class<V, 2>(ctx, a, l, s);
+    auto all = [&](auto stream) {
+        constexpr bool STREAM = decltype(stream)::value;
+        int rc = launch_class<V, STREAM, 0>(ctx, a, l, s);
+        if (rc == HE_OK) rc = launch_class<V, STREAM, 1>(ctx, a, l, s);
+        return rc == HE_OK ? launch_class<V, STREAM, 2>(ctx, a, l, s) : rc;
+    };
+    return stores_stream(l->n_read, l->n_out, limbs, ctx->N, sizeof(V)) ? all(std::true_type{}) : all(std::false_type{});
 }
 
 u64 mul_mod_host(u64 a, u64 b, u64 q) { return (u64)((u128)a * b % q); }
@@ -589,62 +595,164 @@ I8Channel i8_channel(const I8Limb& c, u64 s, int64_t weight_sum, bool packed) {
                      mul_mod_host(s, (mul_mod_host(flipped % q, sum, q) + q - offsets) % q, q)};
 }
 
+namespace {
+
+// Outputs of one or several runs (outputs with the same inputs in the same order), as one group over the union of their inputs.
+struct Merged {
+    struct Run {
+        u32 first, count;
+        std::vector<u32> place;  // of the run's terms in the list; empty: their own order
+    };
+    std::vector<Run> runs;
+    std::vector<u32> list;
+    std::unordered_map<u32, std::vector<u32>> at;  // the places of a ciphertext
+    u32 count = 0;
+
+    // The places of a run's terms; ciphertexts that the list lacks (or has fewer times) are to be appended to it.
+    std::vector<u32> places(const u32* ct, u32 terms, std::vector<u32>& added) const {
+        std::vector<u32> place(terms);
+        std::unordered_map<u32, u32> seen;
+        for (u32 t = 0; t < terms; t++) {
+            const u32 k = seen[ct[t]]++;
+            const auto it = at.find(ct[t]);
+            const u32 have = it == at.end() ? 0 : (u32)it->second.size();
+            if (k < have) {
+                place[t] = it->second[k];
+                continue;
+            }
+            place[t] = (u32)(list.size() + added.size());
+            added.push_back(ct[t]);
+        }
+        return place;
+    }
+    void add(u32 first, u32 n, std::vector<u32> place, const std::vector<u32>& added) {
+        for (u32 ct : added) {
+            at[ct].push_back((u32)list.size());
+            list.push_back(ct);
+        }
+        runs.push_back(Run{first, n, std::move(place)});
+        count += n;
+    }
+};
+
+u32 class_of(u32 count) { return count > 32 ? 2 : count > 16 ? 1 : 0; }
+u32 blocks_of(u32 count, u32 terms) { return count > 32 ? (terms + 63) / 64 * 2 : (terms + 31) / 32; }
+
+// What a group costs, in cycles of a SIMD per 32 slots, as far as it matters for what to merge: loads, transposition and products of a block
+// of terms, the ends of four outputs, and its start.
+u32 group_cost(u32 count, u32 terms) { return blocks_of(count, terms) * (count > 16 ? 700 : 600) + (count + 3) / 4 * 400 + 250; }
+
+struct LayerBuilder {
+    const Rows rows;
+    const int8_t* weights;
+    I8Host& h;
+    std::vector<I8Group> classes[I8_CLASSES];
+    std::unordered_multimap<u64, I8Group> known;  // groups by a hash of their tables, which equal ones share
+
+    u32 add_list(const std::vector<u32>& list, u32 blocks) {
+        const u32 at = (u32)(h.lists.size() / 32);
+        for (u32 t = 0; t < blocks * 32; t++) h.lists.push_back(list[std::min<size_t>(t, list.size() - 1)]);
+        return at;
+    }
+
+    // count outputs from `first` on, whose terms lie at these places of the list (null: in order)
+    void add_group(const Merged& m, u32 first, u32 count, u32 list) {
+        const u32 terms = (u32)m.list.size(), cls = terms == 0 ? 2 : class_of(count), blocks = blocks_of(cls == 2 ? 64 : count, terms);
+        I8Group g{first, count, terms, list, (u32)(h.table.size() / 512), {0, 0, 0}};
+        // First form: [block][tile of 16 rows][lane][8], lane's row lane % 16 (output 4 (row % 4) + row / 4 of the tile), terms 8 (lane / 16) .. of the
+        // block.  Second form: [block][tile of 32 rows][lane][16], row lane % 32, terms 16 (lane / 32) ..
+        const u32 units = cls < 2 ? cls + 1 : 4;  // of 512 bytes, per block
+        const size_t start = h.table.size(), bytes = (size_t)blocks * units * 512;
+        h.table.resize(start + bytes, 0);
+        int8_t* const table = h.table.data() + start;
+        for (const Merged::Run& run : m.runs)
+            for (u32 o = std::max(run.first, first); o < std::min(run.first + run.count, first + count); o++) {
+                const u32 r = o - first, row = r % 4 * 4 + r % 16 / 4, n = rows.terms(o);
+                for (u32 k = 0; k < n; k++) {
+                    const size_t t = run.place.empty() ? k : run.place[k];
+                    const size_t at = cls < 2 ? ((t / 32 * units + r / 16) * 64 + t % 32 / 8 * 16 + row) * 8 + t % 8
+                                              : ((t / 32 * 2 + r / 32) * 64 + t % 32 / 16 * 32 + r % 32) * 16 + t % 16;
+                    table[at] = weights[rows.pt[rows.off[o] + k]];
+                }
+            }
+        u64 hash = 0xCBF29CE484222325ull ^ bytes;
+        for (size_t i = 0; i < bytes; i += 8) {
+            u64 v;
+            memcpy(&v, table + i, 8);
+            hash = (hash ^ v) * 0x100000001B3ull;
+            hash ^= hash >> 29;
+        }
+        const auto range = known.equal_range(hash);
+        bool found = false;
+        for (auto it = range.first; it != range.second && !found; ++it) {
+            const I8Group& k = it->second;
+            const u32 k_cls = k.n_terms == 0 ? 2 : class_of(k.count);
+            if (k_cls != cls || blocks_of(cls == 2 ? 64 : k.count, k.n_terms) != blocks ||
+                (bytes && memcmp(h.table.data() + (size_t)k.table * 512, table, bytes) != 0))
+                continue;
+            g.table = k.table;
+            found = true;
+        }
+        if (found) h.table.resize(start);
+        else known.emplace(hash, g);
+        classes[cls].push_back(g);
+    }
+
+    void flush(Merged& m) {
+        if (m.count) add_group(m, m.runs[0].first, m.count, add_list(m.list, blocks_of(m.count, (u32)m.list.size())));
+        m = Merged();
+    }
+
+    // A run of outputs that is a group or several by itself, all with the same list
+    void add_run(u32 first, u32 end) {
+        const u32 terms = rows.terms(first), tiles = (end - first + 31) / 32, cuts = (tiles + 1) / 2, each = (tiles + cuts - 1) / cuts * 32;
+        Merged m;
+        m.list.assign(rows.ct + rows.off[first], rows.ct + rows.off[first] + terms);
+        m.runs.push_back(Merged::Run{first, end - first, {}});
+        const u32 list = terms ? add_list(m.list, blocks_of(64, terms)) : 0;
+        for (u32 o = first; o < end; o += std::min(each, end - o)) add_group(m, o, std::min(each, end - o), list);
+    }
+
+    // Neighbouring windows of a convolution share most of their inputs: as one group over the union of them (with zeros where a window lacks
+    // one) they are loaded and transposed once, and the tiles of outputs are fuller.
+    void build(u32 n_out) {
+        Merged m;
+        for (u32 o = 0, end; o < n_out; o = end) {
+            end = o + 1;
+            while (end < n_out && rows.same_inputs(o, end)) end++;
+            const u32 n = end - o, terms = rows.terms(o);
+            if (n > 64 || terms == 0) {
+                flush(m);
+                add_run(o, end);
+                continue;
+            }
+            std::vector<u32> added, place = m.places(rows.ct + rows.off[o], terms, added);
+            const u32 joint = (u32)(m.list.size() + added.size());
+            if (m.count && (m.count + n > 32 || group_cost(m.count + n, joint) >= group_cost(m.count, (u32)m.list.size()) + group_cost(n, terms))) {
+                flush(m);
+                added.clear();
+                place = m.places(rows.ct + rows.off[o], terms, added);
+            }
+            m.add(o, n, std::move(place), added);
+        }
+        flush(m);
+    }
+};
+
+}  // namespace
+
 // The host's part of a layer: groups, lists, table and constants (throws std::bad_alloc).
 void build_i8_layer(const he_ctx* ctx, const u32* off, const u32* term_ct, const u32* term_pt, const int8_t* weights, const u64* scale,
                     he_i8_layer* l, I8Host& h) {
-    const Rows rows{off, term_ct, term_pt};
     const u32 n_out = l->n_out;
-    // Runs of outputs that read the same inputs in the same order, cut into groups of up to 64 with the same number of tiles.
-    std::vector<I8Group> classes[I8_CLASSES];
-    std::unordered_multimap<u64, I8Group> known;  // groups by a hash of their weights, to share tables
-    for (u32 o = 0; o < n_out;) {
-        u32 end = o + 1;
-        while (end < n_out && rows.same_inputs(o, end)) end++;
-        const u32 terms = rows.terms(o), pad = end - o > 32 ? 64 : 32, blocks = (terms + pad - 1) / pad * (pad / 32);
-        const u32 tiles = (end - o + 31) / 32, cuts = (tiles + 1) / 2, each = (tiles + cuts - 1) / cuts * 32;
-        const u32 list = (u32)(h.lists.size() / 32);
-        for (u32 t = 0; t < blocks * 32; t++) h.lists.push_back(term_ct[off[o] + std::min(t, terms - 1)]);
-        for (u32 count; o < end; o += count) {
-            count = std::min(each, end - o);
-            I8Group g{o, count, terms, list, 0, {0, 0, 0}};
-            // (outputs without terms go to the second form, whose loop over the blocks may be empty)
-            const u32 cls = count > 32 || terms == 0 ? 2 : count > 16 ? 1 : 0;
-            const size_t n = (size_t)g.count * terms;  // the plaintexts of a group's outputs follow one another
-            u64 hash = 0xCBF29CE484222325ull ^ n;
-            for (size_t i = 0; i < n; i++) hash = (hash ^ term_pt[off[o] + i]) * 0x100000001B3ull;
-            bool found = false;
-            const auto range = known.equal_range(hash);
-            for (auto it = range.first; it != range.second && !found; ++it) {
-                const I8Group& k = it->second;
-                if (k.count != g.count || k.n_terms != terms || (n && memcmp(term_pt + off[k.out0], term_pt + off[o], n * 4) != 0)) continue;
-                g.table = k.table;
-                found = true;
-            }
-            if (!found) {
-                // First form: [block][tile of 16 rows][lane][8], lane's row lane % 16 (output 4 (row % 4) + row / 4 of the tile), terms 8 (lane / 16) .. of the
-                // block.  Second form: [block][tile of 32 rows][lane][16], row lane % 32, terms 16 (lane / 32) ..
-                const u32 units = cls < 2 ? cls + 1 : 4;  // of 512 bytes, per block
-                g.table = (u32)(h.table.size() / 512);
-                h.table.resize(h.table.size() + (size_t)blocks * units * 512, 0);
-                int8_t* t0 = h.table.data() + (size_t)g.table * 512;
-                for (u32 r = 0; r < g.count; r++) {
-                    const u32 row = r % 4 * 4 + r % 16 / 4;
-                    for (u32 t = 0; t < terms; t++) {
-                        const size_t at = cls < 2 ? (((size_t)t / 32 * units + r / 16) * 64 + t % 32 / 8 * 16 + row) * 8 + t % 8
-                                                  : (((size_t)t / 32 * (units / 2) + r / 32) * 64 + t % 32 / 16 * 32 + r % 32) * 16 + t % 16;
-                        t0[at] = weights[term_pt[off[o + r] + t]];
-                    }
-                }
-                known.emplace(hash, g);
-            }
-            classes[cls].push_back(g);
-        }
-    }
+    LayerBuilder b{Rows{off, term_ct, term_pt}, weights, h, {}, {}};
+    b.build(n_out);
     for (u32 cls = 0; cls < I8_CLASSES; cls++) {
         l->class_begin[cls] = (u32)h.groups.size();
-        h.groups.insert(h.groups.end(), classes[cls].begin(), classes[cls].end());
+        h.groups.insert(h.groups.end(), b.classes[cls].begin(), b.classes[cls].end());
     }
     l->class_begin[I8_CLASSES] = (u32)h.groups.size();
+    l->n_read = (u32)std::unordered_set<u32>(term_ct, term_ct + off[n_out]).size();
     // Per limb and output: the scale and the constant that goes with it.
     std::vector<int64_t> weight_sum(n_out);
     for (u32 o = 0; o < n_out; o++)

@@ -168,6 +168,7 @@ struct he_i8_layer {
     he_ctx* ctx;
     int device;
     u32 n_in, n_out, n_terms;
+    u32 n_read;                       // inputs that some term names
     u32 class_begin[I8_CLASSES + 1];  // groups sorted by the tiles of 32 outputs that they take
     I8Limbs limbs;
     I8Group* groups_dev;
@@ -219,9 +220,12 @@ int check_mac_launch(he_ctx* ctx, const he_plan* plan, u32 limbs, int pt_kind);
 // lines costs 256 groups of 16 outputs of one term, N = 2^13, L = 4, 800 us against 540, the layer 30 -> 120 at 2^14, L = 8 (60 + 240 MiB) 322
 // against 301.  What does fit is read from the cache by the call that adds to it or rescales it: the layer 100 -> 200 at 2^13,
 // L = 4 (50 + 100 MiB) 174 us, 181 past the caches; 20 -> 300 with a second call that adds, then the rescale, 296 and 326.
+inline bool stores_stream(u32 n_read, u32 n_out, u32 limbs, u32 N, size_t residue_bytes) {
+    const u64 per_ct = (u64)2 * limbs * N * residue_bytes, out = n_out * per_ct;
+    return out > L2_BYTES && n_read * per_ct + out > MEMORY_CACHE_BYTES;
+}
 inline bool mac_groups_stream(const he_plan* plan, u32 limbs, u32 N, size_t residue_bytes) {
-    const u64 per_ct = (u64)2 * limbs * N * residue_bytes, out = plan->n_out * per_ct;
-    return out > L2_BYTES && plan->n_read * per_ct + out > MEMORY_CACHE_BYTES;
+    return stores_stream(plan->n_read, plan->n_out, limbs, N, residue_bytes);
 }
 // ... and of outputs that share their inputs with no other (64-bit residues), where no rescale follows in the same call: there
 // only if the inputs alone do fit, or sums of three or more terms read them again.  Past the caches and through them, MAC and rescale as
