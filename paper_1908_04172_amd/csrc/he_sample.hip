@@ -8,9 +8,9 @@
 // and the first r tokens of weight v.
 //
 // A workgroup reads its rows once and holds the weights in registers, as many threads per row as that takes (a thread up to 32
-// consecutive tokens).  A cut is found by histograms in the LDS (counts and sums): 8 bins per octave first, then 256 bins of the
-// bin that holds the cut, until that has one element or one value.  The token is found by the running sum in the order
-// of the indices.  Bound by the one reading of the logits where there are many rows.
+// consecutive tokens).  A cut is found from a histogram in the LDS (counts and sums, 8 bins per octave): the bin that holds it, then, if
+// that has more than LIST weights, bins of a 64th of it; what is left is ranked by comparing all with all.  Rows of up to LIST tokens
+// are ranked at once.  The token is found by the running sum in the order of the indices.
 #include <math.h>
 
 #include <algorithm>
@@ -22,8 +22,9 @@ namespace {
 constexpr int ONE_BITS = 47;
 constexpr u64 ONE = 1ull << ONE_BITS;
 constexpr u32 BINS = 384;        // 8 per octave of weights 1 .. 2^47
-constexpr u32 MAX_PER_ROW = 32;  // tokens of a thread
-constexpr u32 MAX_ROWS = 16;     // rows of a workgroup
+constexpr u32 SUB_BITS = 6, SUB_BINS = 1 << SUB_BITS;
+constexpr u32 LIST = 128;
+constexpr u32 MAX_ROWS = 8;      // rows of a workgroup
 
 struct SampleArgs {
     const double* slots;
@@ -37,10 +38,17 @@ struct SampleArgs {
     u32 per;         // tokens of a thread
 };
 
-// A bin: weights base .. base + 2^bits - 1
+// A range of weights, base .. base + 2^bits - 1, and what lies above it.
 struct Bin {
     u64 base, above_sum, sum;
     u32 bits, above_count, count;
+};
+
+// The cut of a row: tokens above `value`, and the first `ties` of those of that weight.
+struct Cut {
+    u64 value;
+    u32 ties;
+    u64 above_sum;
 };
 
 template <u32 T>
@@ -49,6 +57,8 @@ struct Shared {
     u64 sums[2][WAVES][MAX_ROWS];
     u32 counts[2][WAVES][MAX_ROWS];
     Bin found[MAX_ROWS];
+    Cut cut[MAX_ROWS];
+    u32 listed[MAX_ROWS];
 };
 
 // A thread's place among the threads of its row; sums over the row in the order of the threads.
@@ -96,107 +106,154 @@ struct Row {
     }
 };
 
-// The cut of a row: tokens above `value`, and the first `ties` of those of that weight.
-struct Cut {
-    u64 value;
-    u32 ties;
-    u64 above_sum;
+// A workgroup's histograms and lists: entry b of a row at [b * rows + row].
+struct Tables {
+    u64 *sums, *sub_sums, *list;
+    u32 *counts, *sub_counts;
+    __device__ Tables(u64* lds, u32 rows) {
+        sums = lds;
+        list = sub_sums = sums + BINS * rows;  // (the list takes the place of the finer histogram)
+        counts = reinterpret_cast<u32*>(sub_sums + LIST * rows);
+        sub_counts = counts + BINS * rows;
+    }
+    static size_t bytes(u32 rows) { return (size_t)rows * ((BINS + LIST) * sizeof(u64) + (BINS + SUB_BINS) * sizeof(u32)); }
 };
+static_assert(SUB_BINS <= LIST, "");
+
+__device__ __forceinline__ void count_into(u64* sum, u32* count, u64 w) {
+    atomicAdd((unsigned long long*)sum, (unsigned long long)w);
+    atomicAdd(count, 1u);
+}
+
+template <u32 T, int PER>
+__device__ __forceinline__ void octave_histogram(Row<T>& row, const u64 (&w)[PER], const Tables& t) {
+    for (u32 b = threadIdx.x; b < BINS * row.rows; b += T) t.sums[b] = 0, t.counts[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+        if (w[i]) {
+            const u32 e = 63 - __builtin_clzll(w[i]);
+            const u32 bin = (e * 8 + (u32)((w[i] << (63 - e)) >> 60 & 7)) * row.rows + row.row;
+            count_into(&t.sums[bin], &t.counts[bin], w[i]);
+        }
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+}
+
+// Of the bins (the highest first) the one in which the count, or the sum, reaches `target`, into row.sh.found.
+template <bool BY_SUM, u32 T>
+__device__ __forceinline__ void find_bin(Row<T>& row, const u64* sums, const u32* counts, u32 n_bins, u64 target, bool active, const Bin& within) {
+    const u32 each = (n_bins + row.threads - 1) / row.threads, first = row.rank * each, last = min(first + each, n_bins);
+    u64 sum = 0, before, total;
+    u32 count = 0, count_before, count_total;
+    for (u32 k = first; k < last; k++) {
+        sum += sums[(n_bins - 1 - k) * row.rows + row.row];
+        count += counts[(n_bins - 1 - k) * row.rows + row.row];
+    }
+    row.scan(sum, count, before, total, count_before, count_total);
+    before += within.above_sum;
+    count_before += within.above_count;
+    const u64 reached = BY_SUM ? before : count_before;
+    if (active && reached < target && target <= reached + (BY_SUM ? sum : count)) {
+        for (u32 k = first; k < last; k++) {
+            const u32 bin = n_bins - 1 - k;
+            const u64 s = sums[bin * row.rows + row.row];
+            const u32 c = counts[bin * row.rows + row.row];
+            if (target <= (BY_SUM ? before + s : (u64)count_before + c)) {
+                Bin f;
+                if (n_bins == BINS) {
+                    const u32 e = bin / 8;
+                    f.bits = e >= 3 ? e - 3 : 0;
+                    f.base = e >= 3 ? (u64)(8 + bin % 8) << (e - 3) : (8 + bin % 8) >> (3 - e);
+                } else {
+                    f.bits = within.bits > SUB_BITS ? within.bits - SUB_BITS : 0;
+                    f.base = within.base + ((u64)bin << f.bits);
+                }
+                f.above_sum = before;
+                f.above_count = count_before;
+                f.sum = s;
+                f.count = c;
+                row.sh.found[row.row] = f;
+                break;
+            }
+            before += s;
+            count_before += c;
+        }
+    }
+    __syncthreads();
+}
 
 // For the rows with `active`: the cut at which the count (BY_SUM: the sum of the weights) in descending order reaches `target`,
 // 1 <= target <= what the row has.
-template <u32 T, int PER, bool BY_SUM>
-__device__ __forceinline__ void find_cut(Row<T>& row, const u64 (&w)[PER], u64 target, bool active, u64* bin_sum, u32* bin_count, Cut& cut) {
-    u64* sums = bin_sum + row.row;    // bin b of this row: [b * rows]
-    u32* counts = bin_count + row.row;
-    u64 base = 0;
-    u32 bits = 64;                    // 64: the first level, bins of an eighth of an octave
-    u64 above_sum = 0;
-    u32 above_count = 0;
-    while (__syncthreads_or(active)) {
-        for (u32 b = threadIdx.x; b < BINS * row.rows; b += T) bin_sum[b] = 0, bin_count[b] = 0;
-        __syncthreads();
-        const u32 shift = bits == 64 ? 0 : bits > 8 ? bits - 8 : 0;
-        if (active) {
+template <bool BY_SUM, u32 T, int PER>
+__device__ __forceinline__ void find_cut(Row<T>& row, const u64 (&w)[PER], u32 n, u64 target, bool active, const Tables& t, Cut& cut) {
+    if (!__syncthreads_or(active)) return;
+    Bin in{1, 0, 0, 63, 0, n};  // all weights but zero
+    if (n > LIST) {
+        find_bin<BY_SUM>(row, t.sums, t.counts, BINS, target, active, in);
+        if (active) in = row.sh.found[row.row];
+        while (true) {
+            const bool finer = active && in.count > LIST && in.bits > 0;
+            if (!__syncthreads_or(finer)) break;
+            for (u32 b = threadIdx.x; b < SUB_BINS * row.rows; b += T) t.sub_sums[b] = 0, t.sub_counts[b] = 0;
+            __syncthreads();
+            if (finer) {
+                const u32 shift = in.bits > SUB_BITS ? in.bits - SUB_BITS : 0;
 #pragma unroll
-            for (int i = 0; i < PER; i++) {
-                u32 bin;
-                bool in;
-                if (bits == 64) {
-                    const u32 e = 63 - __builtin_clzll(w[i] | 1);
-                    bin = e * 8 + (u32)((e >= 3 ? w[i] >> (e - 3) : w[i] << (3 - e)) & 7);
-                    in = w[i] != 0;
-                } else {
-                    bin = (u32)((w[i] - base) >> shift);
-                    in = w[i] - base < (1ull << bits);  // (wraps below base)
-                }
-                if (in) {
-                    atomicAdd((unsigned long long*)&sums[bin * row.rows], (unsigned long long)w[i]);
-                    atomicAdd(&counts[bin * row.rows], 1u);
-                }
-                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-        __syncthreads();
-        // a thread takes consecutive bins, the highest first
-        const u32 each = (BINS + row.threads - 1) / row.threads, first = row.rank * each;
-        u64 sum = 0, before, total;
-        u32 count = 0, count_before, count_total;
-        for (u32 k = first; k < min(first + each, BINS); k++) {
-            sum += sums[(BINS - 1 - k) * row.rows];
-            count += counts[(BINS - 1 - k) * row.rows];
-        }
-        row.scan(sum, count, before, total, count_before, count_total);
-        before += above_sum;
-        count_before += above_count;
-        const u64 reached = BY_SUM ? before : count_before, after = reached + (BY_SUM ? sum : count);
-        if (active && reached < target && target <= after) {
-            for (u32 k = first; k < min(first + each, BINS); k++) {
-                const u32 bin = BINS - 1 - k;
-                const u64 s = sums[bin * row.rows];
-                const u32 c = counts[bin * row.rows];
-                if (target <= (BY_SUM ? before + s : (u64)count_before + c)) {
-                    Bin f;
-                    if (bits == 64) {
-                        const u32 e = bin / 8;
-                        f.bits = e >= 3 ? e - 3 : 0;
-                        f.base = e >= 3 ? (u64)(8 + bin % 8) << (e - 3) : (8 + bin % 8) >> (3 - e);
-                    } else {
-                        f.bits = shift;
-                        f.base = base + ((u64)bin << shift);
+                for (int i = 0; i < PER; i++) {
+                    if (w[i] - in.base < (1ull << in.bits)) {  // (wraps below base)
+                        const u32 bin = (u32)((w[i] - in.base) >> shift) * row.rows + row.row;
+                        count_into(&t.sub_sums[bin], &t.sub_counts[bin], w[i]);
                     }
-                    f.above_sum = before;
-                    f.above_count = count_before;
-                    f.sum = s;
-                    f.count = c;
-                    row.sh.found[row.row] = f;
-                    break;
+                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
-                before += s;
-                count_before += c;
             }
+            __syncthreads();
+            find_bin<BY_SUM>(row, t.sub_sums, t.sub_counts, SUB_BINS, target, finer, in);
+            if (finer) in = row.sh.found[row.row];
         }
-        __syncthreads();
-        if (active) {
-            const Bin f = row.sh.found[row.row];
-            base = f.base;
-            bits = f.bits;
-            above_sum = f.above_sum;
-            above_count = f.above_count;
-            if (f.count == 1 || bits == 0) {  // one token, or one weight
-                cut.value = f.count == 1 ? f.sum : base;
-                cut.ties = (u32)(BY_SUM ? (target - above_sum + cut.value - 1) / cut.value : target - above_count);
-                cut.above_sum = above_sum;
-                active = false;
+    }
+    // the weights of the range, compared with one another; where they are all the same there is nothing to compare
+    const bool ranked = active && in.bits > 0;
+    if (row.rank == 0) row.sh.listed[row.row] = 0;
+    __syncthreads();
+    if (ranked) {
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            if (w[i] - in.base < (1ull << in.bits)) t.list[atomicAdd(&row.sh.listed[row.row], 1u) * row.rows + row.row] = w[i];
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __syncthreads();
+    if (ranked) {
+        const u32 count = row.sh.listed[row.row];
+        for (u32 i = row.rank; i < count; i += row.threads) {
+            const u64 v = t.list[i * row.rows + row.row];
+            u64 sum = in.above_sum;
+            u32 above = in.above_count, same = 0;
+            for (u32 k = 0; k < count; k++) {
+                const u64 y = t.list[k * row.rows + row.row];
+                sum += y > v ? y : 0;
+                above += y > v;
+                same += y == v;
             }
+            const u64 reached = BY_SUM ? sum : above;
+            if (reached < target && target <= reached + (BY_SUM ? same * v : same))
+                row.sh.cut[row.row] = Cut{v, (u32)(BY_SUM ? (target - sum + v - 1) / v : target - above), sum};
         }
+    }
+    __syncthreads();
+    if (active) {
+        cut = ranked ? row.sh.cut[row.row]
+                     : Cut{in.base, (u32)(BY_SUM ? (target - in.above_sum + in.base - 1) / in.base : target - in.above_count), in.above_sum};
     }
 }
 
 template <u32 T, int PER>
 __global__ void __launch_bounds__(T, 4) sample_kernel(SampleArgs a) {
     __shared__ Shared<T> sh;
-    extern __shared__ u64 bins[];  // [BINS][rows] sums, then counts
+    extern __shared__ u64 lds[];
     Row<T> row(sh, a.rows_log);
     // Workgroups go to the eight XCDs round-robin; neighbouring rows, which may share cache lines, run on one of them.
     const u32 tiles = (a.rows + row.rows - 1) >> a.rows_log, per_xcd = (tiles + 7) / 8;
@@ -205,49 +262,53 @@ __global__ void __launch_bounds__(T, 4) sample_kernel(SampleArgs a) {
     const u32 r = (tile << a.rows_log) + row.row, at = min(r, a.rows - 1);
     const double* col = a.slots + (a.parts == 2 ? at : 2 * (size_t)at);
     const u32 token0 = row.rank * a.per;
+    const int mine = (int)min(a.n, token0 + a.per) - (int)token0;  // this thread's tokens (none: not above zero)
     u64 w[PER];
+    const double* first = col + min(token0, a.n - 1) * a.stride;
+    const int last = max(mine - 1, 0);
+#pragma unroll
+    for (int i = 0; i < PER; i++) {  // (past the end the last one again)
+        w[i] = __builtin_bit_cast(u64, first[(u32)min(i, last) * (u32)a.stride]);
+        if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
     double top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PER; i++) {
-        double x = -INFINITY;
-        if ((u32)i < a.per && token0 + i < a.n) x = col[(token0 + i) * a.stride];
-        w[i] = __builtin_bit_cast(u64, x);
+        if (i >= mine) w[i] = __builtin_bit_cast(u64, (double)-INFINITY);
+        top = fmax(top, __builtin_bit_cast(double, w[i]));  // (NaN never wins)
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int i = 0; i < PER; i++) top = fmax(top, __builtin_bit_cast(double, w[i]));  // (fmax: NaN never wins)
     top = row.max(top);
     const double t = a.temperature ? a.temperature[at] : 1.0;
     const bool greedy = !(t > 0), none = top == -INFINITY;
     const double inv = 1.0 / t;
+    u64 sum = 0, unused, total;
+    u32 some = 0, unused_count, count;
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         const double x = __builtin_bit_cast(double, w[i]);
         // 2^5 has the weight as its mantissa's last 47 bits: one addition rounds it to a whole number
         const double e = greedy ? 0.0 : exp((x - top) * inv);
         w[i] = none ? 0 : x == top ? ONE : e > 0 ? __builtin_bit_cast(u64, e + 32.0) - __builtin_bit_cast(u64, 32.0) : 0;  // (NaN: 0)
+        sum += w[i];
+        some += w[i] != 0;
         if (i % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: the temporaries of all would not fit the registers)
     }
-    u64 unused, total;
-    u32 unused_count, count;
     Cut cut{0, 0, 0};
-    u64* bin_sum = bins;
-    u32* bin_count = reinterpret_cast<u32*>(bins + BINS * row.rows);
-    if (a.top_k || a.top_p) {  // the sum of the weights, and how many are not zero
-        u64 sum = 0;
-        u32 some = 0;
-#pragma unroll
-        for (int i = 0; i < PER; i++) sum += w[i], some += w[i] != 0;
+    if (a.top_k || a.top_p) {
+        const Tables tables(lds, row.rows);
         row.scan(sum, some, unused, total, unused_count, count);
+        if (a.n > LIST) octave_histogram(row, w, tables);
         if (a.top_k) {
             const u32 k = a.top_k[at];
             const bool active = k != 0 && k < count && !greedy && !none;
-            find_cut<T, PER, false>(row, w, k, active, bin_sum, bin_count, cut);
+            find_cut<false>(row, w, a.n, k, active, tables, cut);
             if (active) total = cut.above_sum + cut.ties * cut.value;
         }
         if (a.top_p) {
             const double p = a.top_p[at], need = ceil((double)total * p);
             const u64 target = need >= 1 ? min((u64)need, total) : 1;
-            find_cut<T, PER, true>(row, w, target, p < 1 && !greedy && !none, bin_sum, bin_count, cut);
+            find_cut<true>(row, w, a.n, target, p < 1 && !greedy && !none, tables, cut);
         }
     }
     if (a.min_p && !greedy) {
@@ -255,18 +316,20 @@ __global__ void __launch_bounds__(T, 4) sample_kernel(SampleArgs a) {
         const u64 value = least >= (double)ONE ? ONE : least >= 1 ? (u64)least : 0;  // (the largest weight always stays)
         if (value > cut.value) cut = Cut{value - 1, 0, 0};
     }
-    // the kept weights in the order of the indices
-    u64 sum = 0, before;
+    // the kept weights in the order of the indices: those above the cut, and of those at it the first cut.ties
+    u64 before;
     u32 ties = 0, ties_before;
+    sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         sum += w[i] > cut.value ? w[i] : 0;
         ties += w[i] == cut.value;
     }
-    row.scan(0, ties, unused, unused, ties_before, count);
+    row.scan(sum, ties, before, total, ties_before, count);
+    before += min(ties_before, cut.ties) * cut.value;
+    total += min(count, cut.ties) * cut.value;
     const u32 free = cut.ties > ties_before ? cut.ties - ties_before : 0;  // of this thread's ties the first so many are kept
     sum += min(ties, free) * cut.value;
-    row.scan(sum, 0, before, total, unused_count, count);
     if (r >= a.rows) return;
     if (none) {
         if (row.rank == 0) {
@@ -279,6 +342,7 @@ __global__ void __launch_bounds__(T, 4) sample_kernel(SampleArgs a) {
     const u64 target = place >= 1 ? min(place < 0x1p63 ? (u64)place : total, total - 1) : 0;
     if (before <= target && target < before + sum) {
         u32 token = 0, left = free;
+        asm volatile("" : "+v"(cut.value));  // (the comparisons above are not kept for this)
         u64 run = before;
         bool found = false;
 #pragma unroll
@@ -299,28 +363,34 @@ __global__ void __launch_bounds__(T, 4) sample_kernel(SampleArgs a) {
 template <u32 T, int PER>
 int launch(const SampleArgs& a, int device, hipStream_t s) {
     const u32 rows = 1u << a.rows_log, tiles = (a.rows + rows - 1) / rows;
-    const size_t lds = a.top_k || a.top_p ? (size_t)BINS * rows * (sizeof(u64) + sizeof(u32)) : 0;
     static std::atomic<uint32_t> allowed{0};
-    const int rc = allow_dynamic_lds((const void*)sample_kernel<T, PER>, (size_t)BINS * MAX_ROWS * (sizeof(u64) + sizeof(u32)), device, allowed);
+    const int rc = allow_dynamic_lds((const void*)sample_kernel<T, PER>, Tables::bytes(MAX_ROWS), device, allowed);
     if (rc != HE_OK) return rc;
-    hipLaunchKernelGGL((sample_kernel<T, PER>), dim3((tiles + 7) / 8 * 8), dim3(T), lds, s, a);
+    hipLaunchKernelGGL((sample_kernel<T, PER>), dim3((tiles + 7) / 8 * 8), dim3(T), a.top_k || a.top_p ? Tables::bytes(rows) : 0, s, a);
     HE_HIP(hipGetLastError());
     return HE_OK;
+}
+
+template <u32 T>
+int launch_threads(const SampleArgs& a, int device, hipStream_t s) {  // (a.per is at most 32)
+    return a.per <= 8 ? launch<T, 8>(a, device, s) : a.per <= 16 ? launch<T, 16>(a, device, s) : launch<T, 32>(a, device, s);
 }
 
 }  // namespace
 
 int launch_sample(he_ctx* ctx, const double* slots, u32 n, u32 n_slots, u32 parts, const double* temperature, const u32* top_k, const double* top_p,
                   const double* min_p, const double* uniform, int32_t* tokens, double* log_prob, hipStream_t s) {
-    SampleArgs a{slots, temperature, top_p, min_p, uniform, top_k, tokens, log_prob, (size_t)ctx->N, n, n_slots * parts, parts, 4, 0};
-    const bool wide = n > 512 * MAX_PER_ROW;
-    const u32 T = wide ? 1024 : 512;
-    while (a.rows_log > 0 && ((T >> a.rows_log) * MAX_PER_ROW < n || (a.rows >> a.rows_log) < 256)) a.rows_log--;
+    SampleArgs a{slots, temperature, top_p, min_p, uniform, top_k, tokens, log_prob, (size_t)ctx->N, n, n_slots * parts, parts, 3, 0};
+    // Eight rows, which are a cache line (real parts) or half of one, as far as the registers hold them and there are rows enough for every compute
+    // unit.  A workgroup is no larger than it must be, so that one loads while another searches: rows of 1025 tokens and more take 32 per
+    // thread of 512 (n = 8192, 4096 rows, top-k and top-p: 200 us, with 16 per thread of 1024 295), shorter ones 16 (n = 1000: 50 us, 65 with 32).
+    // Where few rows leave compute units idle, a thread takes eight.
+    const u32 most = n > 1024 ? 32 : 16, widest = n > 512 * 32 ? 1024 : 512;
+    while (a.rows_log > 0 && ((widest >> a.rows_log) * most < n || (a.rows >> a.rows_log) < 256)) a.rows_log--;
+    const bool few = (a.rows >> a.rows_log) < 256;
+    u32 T = 256;
+    while (T < (few ? 1024 : widest) && (T >> a.rows_log) * (few ? 8 : most) < n) T *= 2;
     const u32 threads = T >> a.rows_log;
     a.per = (n + threads - 1) / threads;
-    if (wide) return launch<1024, 32>(a, ctx->device, s);
-    if (a.per <= 4) return launch<512, 4>(a, ctx->device, s);
-    if (a.per <= 8) return launch<512, 8>(a, ctx->device, s);
-    if (a.per <= 16) return launch<512, 16>(a, ctx->device, s);
-    return launch<512, 32>(a, ctx->device, s);
+    return T == 256 ? launch_threads<256>(a, ctx->device, s) : T == 512 ? launch_threads<512>(a, ctx->device, s) : launch_threads<1024>(a, ctx->device, s);
 }
