@@ -136,7 +136,7 @@ def _np32(a) -> np.ndarray:
 
 def _stream() -> int:
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())  # torch.cuda.current_stream().cuda_stream, 2.6 us sooner
 
 
 def _dev_ptr(t, name: str) -> Optional[int]:
@@ -266,13 +266,13 @@ class Context:
         rows = uniform.numel()
         assert slots.dtype == torch.complex128 and half == self.N // 2 and rows % parts == 0
         for t in (uniform, temperature, top_p, min_p, log_prob):
-            assert t is None or (t.dtype == torch.float64 and tuple(t.shape) == (rows,))
-        assert top_k is None or (top_k.dtype == torch.int32 and tuple(top_k.shape) == (rows,))
+            assert t is None or (t.dtype == torch.float64 and t.shape == (rows,))
+        assert top_k is None or (top_k.dtype == torch.int32 and top_k.shape == (rows,))
         if out is None:
             out = torch.empty(rows, dtype=torch.int32, device=slots.device)
         if log_prob is None:
             log_prob = torch.empty(rows, dtype=torch.float64, device=slots.device)
-        assert out.dtype == torch.int32 and tuple(out.shape) == (rows,)
+        assert out.dtype == torch.int32 and out.shape == (rows,)
         _check(lib().he_sample_slots(self._h, _dev_ptr(slots, "slots"), n, rows // parts, parts, _dev_ptr(temperature, "temperature"),
                                      _dev_ptr(top_k, "top_k"), _dev_ptr(top_p, "top_p"), _dev_ptr(min_p, "min_p"),
                                      _dev_ptr(uniform, "uniform"), _dev_ptr(out, "tokens"), _dev_ptr(log_prob, "log_prob"), _stream()),
@@ -382,18 +382,17 @@ class Context:
 
     def _i8_mac(self, name, dtype, layer, ct_in, token_scale, bias, flags, out, workspace):
         import torch
-        limbs = ct_in.shape[2]
-        assert ct_in.dtype == dtype and tuple(ct_in.shape) == (layer.n_in, 2, limbs, self.N)
-        assert token_scale is None or (token_scale.dtype == dtype and tuple(token_scale.shape) == (limbs, self.N))
-        assert bias is None or (bias.dtype == torch.int64 and tuple(bias.shape) == (layer.n_out, limbs))
-        out_limbs = limbs - 1 if flags & RESCALE else limbs
+        n_in, two, limbs, N = ct_in.shape
+        assert ct_in.dtype == dtype and (n_in, two, N) == (layer.n_in, 2, self.N)
+        assert token_scale is None or (token_scale.dtype == dtype and token_scale.shape == (limbs, N))
+        assert bias is None or (bias.dtype == torch.int64 and bias.shape == (layer.n_out, limbs))
+        shape = (layer.n_out, 2, limbs - 1 if flags & RESCALE else limbs, N)
         if out is None:
             assert not flags & ACCUMULATE, "HE_ACCUMULATE adds to an output the caller provides"
-            out = torch.empty((layer.n_out, 2, out_limbs, self.N), dtype=dtype, device=ct_in.device)
-        assert out.dtype == dtype and tuple(out.shape) == (layer.n_out, 2, out_limbs, self.N)
-        if workspace is None:
-            need = layer.workspace_bytes(limbs, flags)
-            workspace = torch.empty(need, dtype=torch.uint8, device=ct_in.device) if need else None
+            out = torch.empty(shape, dtype=dtype, device=ct_in.device)
+        assert out.dtype == dtype and out.shape == shape
+        if workspace is None and flags & RESCALE:
+            workspace = torch.empty(layer.workspace_bytes(limbs, flags), dtype=torch.uint8, device=ct_in.device)
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
         _check(getattr(lib(), name)(self._h, layer._h, limbs, _dev_ptr(ct_in, "ct_in"), _dev_ptr(token_scale, "token_scale"),
                                     _dev_ptr(bias, "bias"), _dev_ptr(out, "ct_out"), flags, _dev_ptr(workspace, "workspace"),
