@@ -41,6 +41,9 @@ enum {
 };
 uint64_t he_host_mac_digits(const uint64_t* x, const uint64_t* w, size_t n, uint64_t q, uint64_t addend, int form);
 uint64_t he_host_digit_reduce(const int32_t* sums, uint64_t q, uint64_t addend, int form);
+/* An output of an int8 layer as the kernels form it: token * (scale * sum of x[t]*w[t]) + bias mod q, from the sums of the residues' bytes;
+ * packed: the 32-bit form (q < 2^30). */
+uint64_t he_host_i8_mac(const uint64_t* x, const int8_t* w, size_t n, uint64_t q, uint64_t scale, uint64_t token, uint64_t bias, int packed);
 /* What the MAC of a fused layer (he_ct_pt_mac with HE_RESCALE) leaves on a kept limb for the rescale kernel: congruent to
  * (sum of x[t]*w[t] + addend) modulo q and below 4q for q < 2^50, else below 6q. */
 uint64_t he_host_mac_accumulate_lazy(const uint64_t* x, const uint64_t* w, size_t n, uint64_t q, uint64_t addend);

@@ -1345,6 +1345,26 @@ uint64_t he_host_mac_digits(const uint64_t* x, const uint64_t* w, size_t n, uint
 
 // What a fused layer's MAC hands to its rescale kernel on a kept limb: unreduced where the limb takes that and the sum is taken
 // in one part, else canonical (longer sums are added up part by part).
+// An output of an int8 layer as the device forms it (he_test.h): digits, their sums, and the end; packed: the 32-bit form.
+uint64_t he_host_i8_mac(const uint64_t* x, const int8_t* w, size_t n, uint64_t q, uint64_t scale, uint64_t token, uint64_t bias, int packed) {
+    I8Limb c;
+    fill_i8_limb(c, q);
+    int64_t weights = 0, digits[8] = {};
+    const u32 half = packed ? 4 : c.nd;
+    for (size_t t = 0; t < n; ++t) {
+        weights += w[t];
+        for (u32 d = 0; d < (packed ? 4 : 2 * half); ++d) digits[d] += (int64_t)w[t] * ((int64_t)(x[t] >> (8 * d) & 255) - 128);
+    }
+    u64 y[2] = {1ull << I8_OFFSET_BITS, 1ull << I8_OFFSET_BITS};
+    for (u32 d = 0; d < 8; ++d) {
+        if (digits[d] != (int32_t)digits[d]) return ~0ull;  // (more terms than a layer takes)
+        if (d < 2 * half) y[d / half] += (u64)(digits[d] * (1ll << (8 * (d % half))));
+    }
+    const I8Channel ch = i8_channel(c, scale, weights, packed);
+    const u64 r = packed ? i8_finish32(y[0], ch, c) : c.exact ? i8_combine<true>(y[0], y[1], ch, c) : i8_combine<false>(y[0], y[1], ch, c);
+    return i8_token(r, token, h_shoup(token, q), bias, c);
+}
+
 uint64_t he_host_mac_accumulate_lazy(const uint64_t* x, const uint64_t* w, size_t n, uint64_t q, uint64_t addend) {
     const LimbConst c = host_const(q);
     const u32 lazy = c.fp_ok ? 2 : mac_lazy(c, HE_MAX_LOG2N - 1);

@@ -395,8 +395,9 @@ HE_HD u32 min_u32(u32 a, u32 b) { return a < b ? a : b; }
 
 // Congruent to y0 s0 + y1 s1 + addend.  With the cheap estimates (each short by at most 2, and the products' companions by 1) below
 // 4q + 4q + q, which fits 64 bits for q < 2^60; else each product is taken below 2q, and the result is below 3q.
-HE_HD u64 i8_combine(u64 y0, u64 y1, const I8Channel& ch, const I8Limb& c) {
-    if (c.exact) {
+template <bool EXACT>
+HE_HD u64 i8_combine(u64 y0, u64 y1, const I8Channel& ch, const I8Limb& c) {  // EXACT: c.exact
+    if constexpr (EXACT) {
         const u64 v = shoup_mul_lazy(y0, ch.s0, ch.s0_shoup, c.q) + shoup_mul_lazy(y1, ch.s1, ch.s1_shoup, c.q);
         return (v >= c.two_q ? v - c.two_q : v) + ch.addend;
     }

@@ -125,19 +125,31 @@ struct End {
     __device__ __forceinline__ u64 half(int32_t s0, int32_t s1, int32_t s2) const { return (u64)((int64_t)s2 * b16 + (int64_t)half(s0, s1)); }
     __device__ __forceinline__ u64 half(int32_t s0, int32_t s1, int32_t s2, int32_t s3) const { return (u64)((int64_t)s3 * b24 + (int64_t)half(s0, s1, s2)); }
 
-    // an output, from the sums of its halves at the two units
+    // f with the parameters of store
+    template <int ND, typename F>
+    __device__ __forceinline__ void with_kind(F f) const {
+        using yes = std::true_type;
+        using no = std::false_type;
+        if constexpr (ND == 4 && sizeof(V) == 8) {  // (q >= 2^60 has eight bytes)
+            if (c.exact) return has_token ? f(yes{}, yes{}) : f(yes{}, no{});
+        }
+        has_token ? f(no{}, yes{}) : f(no{}, no{});
+    }
+    // An output, from the sums of its halves at the two units.  (What no output of a call differs in is a parameter: a branch around every product
+    // keeps those of the two units apart, each a chain that waits for itself.)
+    template <bool EXACT, bool TOKEN>
     __device__ __forceinline__ void store(V* p, const Ends& e, const u64 (&y0)[2], const u64 (&y1)[2]) const {
         typedef V piece __attribute__((ext_vector_type(SLOTS), aligned(8)));  // 16 bytes (see u64x2)
         piece v;
 #pragma unroll
         for (int k = 0; k < 2; k++) {
             if constexpr (sizeof(V) == 8) {
-                const u64 r = i8_combine(y0[k], y1[k], e.ch, c);
-                v[k] = has_token ? i8_token(r, tok[k], tok_shoup[k], e.bias, c) : i8_reduce(r, c);
+                const u64 r = i8_combine<EXACT>(y0[k], y1[k], e.ch, c);
+                v[k] = TOKEN ? i8_token(r, tok[k], tok_shoup[k], e.bias, c) : i8_reduce(r, c);
             } else {  // the halves are two slots
                 v[2 * k] = i8_finish32(y0[k], e.ch, c);
                 v[2 * k + 1] = i8_finish32(y1[k], e.ch, c);
-                if (has_token) {
+                if constexpr (TOKEN) {
                     v[2 * k] = (u32)i8_token(v[2 * k], tok[2 * k], tok_shoup[2 * k], e.bias, c);
                     v[2 * k + 1] = (u32)i8_token(v[2 * k + 1], tok[2 * k + 1], tok_shoup[2 * k + 1], e.bias, c);
                 }
@@ -291,26 +303,28 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
             const I8Group g = load_group(a.groups + a.first + cur.group);
             const Ends* ends = lds + (cur.group - begin) * 16 * RT;
             V* const dst = dst0 + g.out0 * out_stride;
+            fin.template with_kind<ND>([&](auto exact, auto token) {
 #pragma unroll
-            for (int i = 0; i < 4 * RT; i++) {
-                if (4 * (u32)i >= g.count) break;
-                const u32 mine = 4 * i + quarter;
-                if (mine < g.count) {
-                    u64 y[2][2];
+                for (int i = 0; i < 4 * RT; i++) {
+                        if (4 * (u32)i >= g.count) break;
+                    const u32 mine = 4 * i + quarter;
+                    if (mine < g.count) {
+                        u64 y[2][2];
 #pragma unroll
-                    for (int h = 0; h < 2; h++)
+                        for (int h = 0; h < 2; h++)
 #pragma unroll
-                        for (int k = 0; k < 2; k++) {
-                            const v4i (&t)[2 * ND] = sums[i / 4][k];
-                            const int r = i % 4;
-                            if constexpr (ND == 2) y[h][k] = fin.half(t[2 * h][r], t[2 * h + 1][r]);
-                            else if constexpr (ND == 3) y[h][k] = fin.half(t[3 * h][r], t[3 * h + 1][r], t[3 * h + 2][r]);
-                            else y[h][k] = fin.half(t[4 * h][r], t[4 * h + 1][r], t[4 * h + 2][r], t[4 * h + 3][r]);
-                        }
-                    fin.store(dst + mine * out_stride, ends[mine], y[0], y[1]);
+                            for (int k = 0; k < 2; k++) {
+                                const v4i (&t)[2 * ND] = sums[i / 4][k];
+                                const int r = i % 4;
+                                if constexpr (ND == 2) y[h][k] = fin.half(t[2 * h][r], t[2 * h + 1][r]);
+                                else if constexpr (ND == 3) y[h][k] = fin.half(t[3 * h][r], t[3 * h + 1][r], t[3 * h + 2][r]);
+                                else y[h][k] = fin.half(t[4 * h][r], t[4 * h + 1][r], t[4 * h + 2][r], t[4 * h + 3][r]);
+                            }
+                        fin.template store<decltype(exact)::value, decltype(token)::value>(dst + mine * out_stride, ends[mine], y[0], y[1]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);           // one output at a time: its temporaries are few
                 }
-                __builtin_amdgcn_sched_barrier(0);           // one output at a time: its temporaries are few
-            }
+            });
             if (cur.group + 1 >= end) break;
         }
         cur = nxt;
@@ -423,11 +437,12 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
                 if (q < 3) in[d] = from[(((q + 1) / 2 * 8 + d) * 2 + (q + 1) % 2) * 64];
             }
             write_operand(to, x[P ^ 1], q % 2, q / 2);
+            // a product, an operand of the next fourth and a share of the arithmetic in turn (in any other order six registers too many are alive)
 #pragma unroll
             for (int d = 0; d < ND; d++) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product,
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an operand of the next fourth,
-                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);  // and a share of the arithmetic behind them
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -466,7 +481,7 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
         else return fin.half(t[0][r], t[1][r], t[2][r], t[3][r]);
     };
     // The wavefront of the lower digits finishes the first eight of a lane's outputs, the other one the last eight: they exchange the others' sums.
-    auto finish = [&](auto of_upper) {
+    auto finish = [&](auto of_upper, auto exact, auto token) {
         constexpr bool UPPER = decltype(of_upper)::value;
         constexpr int KEEP = UPPER ? 8 : 0, SEND = 8 - KEEP;
         u64* exchange = reinterpret_cast<u64*>(lds) + lane;  // [wavefront][output][column tile][lane]
@@ -480,13 +495,15 @@ __device__ __forceinline__ void split_body(const I8Args<V>& a, const LimbConst& 
                 u64 own_sum[2], other[2];
 #pragma unroll
                 for (int k = 0; k < 2; k++) own_sum[k] = sum(k, KEEP + i), other[k] = exchange[((wave ^ 1) * 16 + 2 * i + k) * 64];
-                fin.store(dst + mine * out_stride, ends[mine], UPPER ? other : own_sum, UPPER ? own_sum : other);
+                fin.template store<decltype(exact)::value, decltype(token)::value>(dst + mine * out_stride, ends[mine], UPPER ? other : own_sum, UPPER ? own_sum : other);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    if (upper) finish(std::true_type{});
-    else finish(std::false_type{});
+    fin.template with_kind<ND>([&](auto exact, auto token) {
+        if (upper) finish(std::true_type{}, exact, token);
+        else finish(std::false_type{}, exact, token);
+    });
 }
 
 template <typename V, bool STREAM>

@@ -37,7 +37,7 @@ EXPORTS = [
     "he_host_mac_accumulate", "he_host_mac_accumulate_add", "he_host_mac_accumulate_lazy", "he_test_mac_for_rescale", "he_measure_rate",
     "he_host_barrett64", "he_host_shoup32", "he_host_mac_digits", "he_host_digit_reduce", "he_test_mac_groups_per_workgroup", "he_test_mac_form", "he_host_ntt_forward_fp64", "he_host_ntt_expand_fp64", "he_host_ntt_inverse_fp64", "he_test_integer_transforms", "he_square_relin_workspace_bytes", "he_ct_square_relin", "he_pack32", "he_unpack32", "he_ct_pt_mac32", "he_ct_pt_add32", "he_rescale32", "he_ntt_fwd32", "he_ntt_inv32",
     "he_i8_layer_create", "he_i8_layer_destroy", "he_i8_workspace_bytes", "he_ct_i8_mac", "he_ct_i8_mac32",
-    "he_sample_slots",
+    "he_sample_slots", "he_host_i8_mac",
 ]
 
 _lib = None
@@ -110,6 +110,7 @@ def lib():
         "he_i8_layer_destroy": (i32, [vp]),
         "he_i8_workspace_bytes": (i32, [vp, u32, u32, ctypes.POINTER(sz)]),
         "he_ct_i8_mac": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
+        "he_host_i8_mac": (u64, [vp, vp, sz, u64, u64, u64, u64, i32]),
         "he_sample_slots": (i32, [vp, vp, u32, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp]),
         "he_ct_i8_mac32": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
     }
@@ -587,6 +588,13 @@ class I8Layer:
 
 
 # -- host-side checks of the device arithmetic
+
+def host_i8_mac(x, w, q: int, scale: int = 1, token: int = 1, bias: int = 0, packed: bool = False) -> int:
+    """he_host_i8_mac: token * (scale * sum of x*w) + bias mod q."""
+    x, w = _np64(x), np.ascontiguousarray(w, dtype=np.int8)
+    assert x.shape == w.shape
+    return int(lib().he_host_i8_mac(x.ctypes.data, w.ctypes.data, x.size, q, scale, token, bias, int(packed)))
+
 
 def host_mulmod(a: int, b: int, q: int) -> int:
     return int(lib().he_host_mulmod(a, b, q))
