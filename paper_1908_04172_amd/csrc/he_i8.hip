@@ -18,6 +18,13 @@
 // Residues in packed storage are taken two at a time as one of eight bytes (first form), or one half alone (second).
 //
 // The end of an output, two products by constants of the output and one reduction: I8Channel in he_arith.h.
+//
+// What bounds it: the first form the vector ALU, whose instructions are 30 % transposition and 70 % ends (a 16x16x8 map, 3x3x16, N = 2^13, L = 3,
+// with tokens: 863 us for 2.4 GB; a 28x28 image, 5x5x5, L = 4: 206 us for 0.79 GB, 3.8 TB/s); long sums over few groups the inputs' way from memory (845 -> 100 at
+// 2^13, L = 4: 124 us for 0.50 GB, 4.0 TB/s; he_ct_pt_mac's products alone 345 us); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2: 102 us),
+// of long ones the products, transposition and LDS in turn (1024 -> 1024 packed: 122 us, 1.1 int8 POP/s).
+// Groups of the second form hold 64 outputs and not 128, whose sums would leave one workgroup per compute unit, with its ends in the open: 256 -> 1000 106 and
+// 150 us, 845 -> 100 142 and 161, 1024 -> 1024 packed 134 and 140.
 #include <string.h>
 
 #include <algorithm>
@@ -34,11 +41,12 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 constexpr u32 THREADS = 256;
-constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most
+constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most (the 16x16x8 map 968 us, 1016 with two)
 constexpr u64 MIN_WORKGROUPS = 2048; // ... while the launch keeps at least this many workgroups
-constexpr u64 SMALL_LAUNCH = 512;    // workgroups
 
-// slots of 64 units of eight bytes, a workgroup of the second form
+// slots of a workgroup, in units of eight bytes: 32 per wavefront in the first form, 64 in all in the second
+template <typename V>
+__host__ __device__ constexpr u32 whole_slots() { return THREADS / 2 * 8 / sizeof(V); }
 template <typename V>
 __host__ __device__ constexpr u32 split_slots() { return 64 * 8 / sizeof(V); }
 
@@ -223,13 +231,13 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
     const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64, quarter = lane / 16, col = lane % 16;
     constexpr u32 PER = 8 / sizeof(V);                       // residues of a unit
     const u32 comp = row & 1, limb = row >> 1;
-    const u32 slot = (part * blockDim.x / 2 + wave * 32 + col * 2) * PER;
+    const u32 slot = part * whole_slots<V>() + (wave * 32 + col * 2) * PER;
     const size_t at = ((size_t)comp * a.limbs + limb) * a.N + slot;
     const u32 ct_stride = 2 * a.limbs * a.N * sizeof(V);     // bytes
     const char* x_base = reinterpret_cast<const char*>(a.ct_in + at);
     const size_t out_stride = (size_t)2 * a.limbs * a.N;
     V* const dst0 = a.out + at;
-    for (u32 i = threadIdx.x; i < (end - begin) * 16 * RT; i += blockDim.x) {
+    for (u32 i = threadIdx.x; i < (end - begin) * 16 * RT; i += THREADS) {
         const I8Group& g = a.groups[a.first + begin + i / (16 * RT)];
         if (i % (16 * RT) < g.count) lds[i] = ends_of(a, row, g.out0 + i % (16 * RT), lc.q);
     }
@@ -349,7 +357,7 @@ __device__ __forceinline__ Place place_of(u32 parts, u32 runs) {
 template <typename V, int RT, bool STREAM>
 __global__ void __launch_bounds__(THREADS, 2) i8_whole_kernel(LimbTable lt, I8Limbs lc, I8Args<V> a) {
     __shared__ Ends lds[WHOLE_RUN * 16 * RT];
-    const Place at = place_of(a.N / (blockDim.x * 4 / sizeof(V)), a.runs);
+    const Place at = place_of(a.N / whole_slots<V>(), a.runs);
     const u32 begin = at.run * a.run, end = min(begin + a.run, a.n_groups);
     const LimbConst& c = lt.c[at.row >> 1];
     const I8Limb& l = lc.c[at.row >> 1];
@@ -524,20 +532,18 @@ __global__ void __launch_bounds__(THREADS, 2) i8_split_kernel(LimbTable lt, I8Li
 template <typename V>
 u32 class_count(const he_i8_layer* l, u32 cls) { return l->class_begin[cls + 1] - l->class_begin[cls]; }
 
-// How a class is launched: the groups that a workgroup takes, its threads, and the workgroups.
+// How a class is launched: the groups that a workgroup takes, and the workgroups.
 struct Launch {
-    u32 run, threads;
+    u32 run;
     u64 blocks;
 };
 template <typename V>
 Launch class_launch(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls) {
     const u64 rows = 2 * limbs, count = class_count<V>(l, cls);
-    if (cls >= 2) return Launch{1, THREADS, count * (ctx->N / split_slots<V>()) * rows};
-    // The first form's wavefronts are independent: a small launch has one per workgroup, to reach every compute unit.
-    Launch k{WHOLE_RUN, THREADS, 0};
-    auto blocks = [&] { return (count + k.run - 1) / k.run * (ctx->N / (k.threads * 4 / sizeof(V))) * rows; };
+    if (cls >= 2) return Launch{1, count * (ctx->N / split_slots<V>()) * rows};
+    Launch k{WHOLE_RUN, 0};
+    auto blocks = [&] { return (count + k.run - 1) / k.run * (ctx->N / whole_slots<V>()) * rows; };
     while (k.run > 1 && blocks() < MIN_WORKGROUPS) k.run /= 2;
-    if (blocks() < SMALL_LAUNCH) k.threads = 64;
     k.blocks = blocks();
     return k;
 }
@@ -548,7 +554,7 @@ int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) 
     a.n_groups = class_count<V>(l, CLS);
     if (a.n_groups == 0) return HE_OK;
     const Launch k = class_launch<V>(ctx, l, a.limbs, CLS);
-    const dim3 grid((u32)k.blocks), block(k.threads);
+    const dim3 grid((u32)k.blocks), block(THREADS);
     a.run = k.run;
     a.runs = (a.n_groups + a.run - 1) / a.run;
     if constexpr (CLS < 2) hipLaunchKernelGGL((i8_whole_kernel<V, CLS + 1, STREAM>), grid, block, 0, s, ctx->limbs, l->limbs, a);
@@ -652,6 +658,8 @@ struct Merged {
     }
 };
 
+// The classes of groups: one or two tiles of 16 in the first form, two of 32 in the second.  (One tile is half the products: 845 -> 10 at N = 2^13, L = 4,
+// 78.9 us, 80.4 with two.)
 u32 class_of(u32 count) { return count > 32 ? 2 : count > 16 ? 1 : 0; }
 u32 blocks_of(u32 count, u32 terms) { return count > 32 ? (terms + 63) / 64 * 2 : (terms + 31) / 32; }
 

@@ -11,6 +11,10 @@
 // consecutive tokens).  A cut is found from a histogram in the LDS (counts and sums, 8 bins per octave): the bin that holds it, then, if
 // that has more than LIST weights, bins of a 64th of it; what is left is ranked by comparing all with all.  Rows of up to LIST tokens
 // are ranked at once.  The token is found by the running sum in the order of the indices.
+//
+// What bounds it: long rows the loads, of which a workgroup of two rows takes 16 bytes of every line (8192 tokens, 4096 rows, top-k and top-p: 200 us for
+// 268 MB, 125 without filters); shorter ones the histogram's atomics and the meetings of the wavefronts (1000 tokens, 4096 rows, all filters: 48 us, 22 without); few rows and
+// short ones latency (5003 tokens, 37 rows: 26 us; ten tokens, 2048 rows: 6 us).
 #include <math.h>
 
 #include <algorithm>
@@ -23,7 +27,7 @@ constexpr int ONE_BITS = 47;
 constexpr u64 ONE = 1ull << ONE_BITS;
 constexpr u32 BINS = 384;        // 8 per octave of weights 1 .. 2^47
 constexpr u32 SUB_BITS = 6, SUB_BINS = 1 << SUB_BITS;
-constexpr u32 LIST = 128;
+constexpr u32 LIST = 128;        // weights that are ranked by comparing all with all
 constexpr u32 MAX_ROWS = 8;      // rows of a workgroup
 
 struct SampleArgs {

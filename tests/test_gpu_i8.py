@@ -299,3 +299,45 @@ def test_refusals_on_a_device(he):
     assert status(lambda: layer_of(ctx, plan, w, np.array([1.0, np.inf, 1.0]))) == -1
     empty = ctx.i8_layer(5, 0, 15, np.zeros(1, np.uint32), [], [], w)
     assert ctx.ct_i8_mac(empty, x).numel() == 0
+
+
+def test_arrays_at_odd_multiples_of_eight_bytes(he):
+    N = 1 << 11
+
+    def shifted(t):
+        raw = torch.empty(t.numel() * t.element_size() + 8, dtype=torch.uint8, device="cuda")
+        view = raw[8:].view(t.dtype).view(t.shape)
+        assert view.data_ptr() % 16 == 8
+        view.copy_(t)
+        return view
+
+    for bits, M in (([60, 40], 9), ([60, 40], 50), ([30, 30], 9), ([30, 30], 50)):
+        q = wl.modulus_chain(bits, N)
+        ctx = he.Context(11, q)
+        plan = wl.dense_plan(40, M)
+        ct, w, scale, token, b = operands(plan, q, N, M)
+        layer = layer_of(ctx, plan, w, scale, 2.0**20)
+        x, tok, bias = dev(ct), dev(token), dev(b)
+        call = ctx.ct_i8_mac
+        if bits[0] == 30:
+            x, tok, call = ctx.pack32(x), ctx.pack32(tok), ctx.ct_i8_mac32
+        for flags in (0, he.RESCALE):
+            want = call(layer, x, tok, bias, flags=flags)
+            ws = torch.empty(layer.workspace_bytes(2, flags) + 8, dtype=torch.uint8, device="cuda")[8:] if flags else None
+            got = call(layer, shifted(x), shifted(tok), shifted(bias), flags=flags, out=shifted(torch.zeros_like(want)), workspace=ws)
+            assert torch.equal(got, want)
+
+
+def test_single_outputs_share_blocks_of_terms(he):
+    """An elementwise scaling and a depthwise convolution: outputs with inputs of their own, which the layer merges."""
+    N, n = 1 << 10, 75
+    q = wl.modulus_chain([60, 50], N)
+    ctx = he.Context(10, q)
+    each = np.arange(n, dtype=np.uint32)
+    scaling = wl.Plan(n, n, n, np.arange(n + 1, dtype=np.uint32), each, each)
+    taps = np.stack([np.clip(each.astype(int) + d, 0, n - 1) for d in (-1, 0, 1)], 1).astype(np.uint32)  # (the ends read an input twice)
+    depthwise = wl.Plan(n, n, 3, np.arange(n + 1, dtype=np.uint32) * 3, taps.ravel(), np.tile(np.arange(3, dtype=np.uint32), n))
+    for plan in (scaling, depthwise):
+        ct, w, scale, token, b = operands(plan, q, N, 31, extreme=True)
+        got = ctx.ct_i8_mac(layer_of(ctx, plan, w, scale, 2.0**25), dev(ct), dev(token), dev(b))
+        assert np.array_equal(host(got), expected(ct, q, plan, w, scale, 2.0**25, token, b))

@@ -249,3 +249,34 @@ def test_streams_and_a_captured_graph(contexts):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(tokens, eager[0]) and torch.equal(log_prob, eager[1])
+
+
+def test_arrays_at_odd_multiples_of_eight_bytes(contexts):
+    ctx = contexts(10)
+
+    def shifted(t):
+        raw = torch.empty(t.numel() * t.element_size() + 8, dtype=torch.uint8, device="cuda")
+        view = raw[8:].view(t.dtype).view(t.shape)
+        view.copy_(t)
+        return view
+
+    flat = torch.randn(200 * 1024 + 1, dtype=torch.float64, device="cuda")[1:].view(200, 512, 2)
+    slots = torch.view_as_complex(flat.clone())
+    odd = torch.empty(200 * 512 * 16 + 8, dtype=torch.uint8, device="cuda")[8:].view(torch.float64).view(200, 512, 2)
+    odd.copy_(flat)
+    u = torch.rand(1024, dtype=torch.float64, device="cuda")
+    p = torch.full_like(u, 0.8)
+    want = ctx.sample_slots(slots, u, parts=2, top_p=p)
+    lib, ptr = ctx_lib(), lambda t: t.data_ptr()
+    tokens, log_prob = shifted(torch.zeros_like(want[0])), shifted(torch.zeros_like(want[1]))
+    odd_p, odd_u = shifted(p), shifted(u)
+    assert all(ptr(t) % 16 == 8 for t in (odd, odd_p, odd_u, log_prob))
+    status = lib.he_sample_slots(ctx._h, ptr(odd), 200, 512, 2, None, None, ptr(odd_p), None, ptr(odd_u), ptr(tokens), ptr(log_prob),
+                                 torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert status == 0 and torch.equal(tokens, want[0]) and torch.equal(log_prob, want[1])
+
+
+def ctx_lib():
+    from paper_1908_04172_amd import he
+    return he.lib()
