@@ -265,9 +265,10 @@ int he_ct_square_relin(he_ctx* ctx, uint32_t limbs, const uint64_t* ct_in, uint3
  *
  * he_i8_layer_create: arrays as in he_plan_create; weights host [n_pt], channel_scale host [n_out] or NULL (non-finite products:
  * HE_ERR_ARG); all are copied, laid out for the kernels and kept on the context's GPU.  A layer serves every level.  At most
- * 131071 terms per output (HE_ERR_RANGE; longer sums go over several layers with HE_ACCUMULATE).  Takes device memory of about
- * 32 bytes per term and group of up to 32 outputs with the same inputs (groups with the same weights share it), and 48 bytes per
- * output and limb.  he_i8_layer_destroy is valid also after the context was destroyed.
+ * 131071 terms per output (HE_ERR_RANGE; longer sums go over several layers with HE_ACCUMULATE).  Outputs that follow one another and read the
+ * same ciphertexts, or mostly the same (neighbouring windows of a convolution), are grouped, at most 64; a group takes device memory of a byte per
+ * term and output (terms rounded up to 32 or 64, outputs to 16, 32 or 64; groups with the same weights share it) and four
+ * per term, and the layer 80 bytes per output and limb.  he_i8_layer_destroy is valid also after the context was destroyed.
  *
  * he_ct_i8_mac: ct_in, ct_out, bias, flags, workspace and the rule against overlaps as in he_ct_pt_mac (he_i8_workspace_bytes: the
  * accumulators with HE_RESCALE, else 0, and then workspace may be NULL).

@@ -3,6 +3,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <map>
 #include <mutex>
 #include <new>
@@ -1045,7 +1046,7 @@ int he_i8_layer_create(he_ctx* ctx, uint32_t n_in, uint32_t n_out, uint32_t n_pt
             upload(&l->table_dev, h.table.data(), h.table.size()) != HE_OK || upload(&l->channels_dev, h.channels.data(), h.channels.size()) != HE_OK ||
             upload(&l->channels32_dev, h.channels32.data(), h.channels32.size()) != HE_OK)
             rc = HE_ERR_DEVICE;
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {  // (too little host memory)
         rc = HE_ERR_RANGE;
     }
     if (rc != HE_OK) {

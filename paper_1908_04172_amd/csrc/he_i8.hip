@@ -20,9 +20,9 @@
 // The end of an output, two products by constants of the output and one reduction: I8Channel in he_arith.h.
 //
 // What bounds it: the first form the vector ALU, whose instructions are 30 % transposition and 70 % ends (a 16x16x8 map, 3x3x16, N = 2^13, L = 3,
-// with tokens: 863 us for 2.4 GB; a 28x28 image, 5x5x5, L = 4: 206 us for 0.79 GB, 3.8 TB/s); long sums over few groups the inputs' way from memory (845 -> 100 at
-// 2^13, L = 4: 124 us for 0.50 GB, 4.0 TB/s; he_ct_pt_mac's products alone 345 us); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2: 102 us),
-// of long ones the products, transposition and LDS in turn (1024 -> 1024 packed: 122 us, 1.1 int8 POP/s).
+// with tokens: 833 us for 2.4 GB; a 28x28 image, 5x5x5, L = 4: 205 us for 0.79 GB, 3.8 TB/s); long sums over few groups the inputs' way from memory (845 -> 100 at
+// 2^13, L = 4: 122 us for 0.50 GB, 4.1 TB/s; he_ct_pt_mac's products alone 345 us); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2: 101 us),
+// of long ones the products, transposition and LDS in turn (1024 -> 1024 packed: 115 us, 1.2 int8 POP/s).
 // Groups of the second form hold 64 outputs and not 128, whose sums would leave one workgroup per compute unit, with its ends in the open: 256 -> 1000 106 and
 // 150 us, 845 -> 100 142 and 161, 1024 -> 1024 packed 134 and 140.
 #include <string.h>

@@ -12,8 +12,8 @@
 // that has more than LIST weights, bins of a 64th of it; what is left is ranked by comparing all with all.  Rows of up to LIST tokens
 // are ranked at once.  The token is found by the running sum in the order of the indices.
 //
-// What bounds it: long rows the loads, of which a workgroup of two rows takes 16 bytes of every line (8192 tokens, 4096 rows, top-k and top-p: 200 us for
-// 268 MB, 125 without filters); shorter ones the histogram's atomics and the meetings of the wavefronts (1000 tokens, 4096 rows, all filters: 48 us, 22 without); few rows and
+// What bounds it: long rows the loads, of which a workgroup of two rows takes 16 bytes of every line, and the vector ALU in turn (8192 tokens, 4096 rows, top-k and
+// top-p: 200 us for 268 MB, 125 without filters); shorter ones the histogram's atomics and the meetings of the wavefronts (1000 tokens, 4096 rows, all filters: 48 us, 22 without); few rows and
 // short ones latency (5003 tokens, 37 rows: 26 us; ten tokens, 2048 rows: 6 us).
 #include <math.h>
 
