@@ -341,3 +341,23 @@ def test_single_outputs_share_blocks_of_terms(he):
         ct, w, scale, token, b = operands(plan, q, N, 31, extreme=True)
         got = ctx.ct_i8_mac(layer_of(ctx, plan, w, scale, 2.0**25), dev(ct), dev(token), dev(b))
         assert np.array_equal(host(got), expected(ct, q, plan, w, scale, 2.0**25, token, b))
+
+
+@pytest.mark.parametrize("terms", [2047, 2048, 2049, 2112, 4160])
+def test_large_groups_whose_lists_are_taken_in_parts(he, terms):
+    """More terms than the list in the LDS holds at a time, in both storage forms."""
+    N = 1 << 10
+    q = wl.modulus_chain([30, 27], N)
+    ctx = he.Context(10, q)
+    plan = groups_plan([(40, terms)], 60, 70, terms)
+    ct, w, scale, token, b = operands(plan, q, N, terms, extreme=True)
+    layer = layer_of(ctx, plan, w, scale, 2.0**20)
+    want = expected(ct, q, plan, w, scale, 2.0**20, token, b)
+    assert np.array_equal(host(ctx.ct_i8_mac(layer, dev(ct), dev(token), dev(b))), want)
+    got = ctx.ct_i8_mac32(layer, ctx.pack32(dev(ct)), ctx.pack32(dev(token)), dev(b))
+    assert np.array_equal(host(ctx.unpack32(got)), want)
+    q60 = wl.modulus_chain([62], N)                                 # four digits a half, the exact estimates
+    ctx60 = he.Context(10, q60)
+    ct, w, scale, _, b = operands(plan, q60, N, terms + 1)
+    got = ctx60.ct_i8_mac(layer_of(ctx60, plan, w, scale, 2.0**30), dev(ct), bias=dev(b))
+    assert np.array_equal(host(got), expected(ct, q60, plan, w, scale, 2.0**30, None, b))
