@@ -140,13 +140,25 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())  # torch.cuda.current_stream().cuda_stream, 2.6 us sooner
 
 
+_Tensor = _DTYPES = None  # torch's tensors, and of each dtype that the calls take whether torch conjugates or negates it lazily
+
+
 def _dev_ptr(t, name: str) -> Optional[int]:
     if t is None:
         return None
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+    global _Tensor, _DTYPES
+    if _Tensor is None:
+        import torch
+        _Tensor = torch.Tensor
+        _DTYPES = {torch.int64: False, torch.int32: False, torch.uint8: False, torch.float64: True, torch.complex128: True}
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a contiguous CUDA tensor")
-    if t.dtype not in (torch.int64, torch.int32, torch.float64, torch.uint8, torch.complex128):
+    lazy = _DTYPES.get(t.dtype)
+    if lazy and (t.is_neg() or t.is_conj()):  # (the memory holds other values than the tensor)
+        raise TypeError(f"{name} is lazily conjugated or negated: call resolve_conj() or resolve_neg() first")
+    if not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous CUDA tensor")
+    if lazy is None:
         raise TypeError(f"{name}: unexpected dtype {t.dtype}")
     return t.data_ptr()
 
