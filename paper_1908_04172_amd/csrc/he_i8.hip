@@ -589,10 +589,10 @@ struct Rows {
 
 }  // namespace
 
-// every launch of a call must fit a grid
+// every launch of a call must fit a grid, whose threads HIP counts in 32 bits
 int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed) {
     for (u32 cls = 0; cls < I8_CLASSES; cls++)
-        if ((packed ? class_launch<u32>(ctx, l, limbs, cls) : class_launch<u64>(ctx, l, limbs, cls)).blocks > 0x7FFFFFFFull) return HE_ERR_RANGE;
+        if ((packed ? class_launch<u32>(ctx, l, limbs, cls) : class_launch<u64>(ctx, l, limbs, cls)).blocks * THREADS > 0xFFFFFFFFull) return HE_ERR_RANGE;
     return HE_OK;
 }
 
