@@ -94,6 +94,13 @@ enum {
 int he_test_mac_form(const he_plan* plan, uint32_t limbs, uint32_t outputs, int packed, uint32_t flags, uint32_t* form);
 
 /*
+ * How he_ct_i8_mac (packed: he_ct_i8_mac32) launches the layer's groups of up to 16, 32 or 64 outputs (outputs: 1 .. 16, 17 .. 32, 33 .. 64;
+ * outputs without terms go with the last) at this level: how many groups they are, how many of them a workgroup runs through
+ * at most, and whether the outputs are written past the caches (HE_FORM_PAST_CACHES).
+ */
+int he_test_i8_form(const he_i8_layer* layer, uint32_t limbs, uint32_t outputs, int packed, uint32_t* groups, uint32_t* run, uint32_t* form);
+
+/*
  * The transforms of limbs below 2^50 run on double-precision FMAs, those of larger limbs on integer butterflies; both
  * produce the same residues.  integer_only = 1 makes every later call on this context use the integer butterflies for
  * all limbs (for tests of those butterflies on such limbs, and for timing one arithmetic against the other);

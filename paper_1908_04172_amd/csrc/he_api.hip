@@ -1404,6 +1404,16 @@ int he_test_mac_form(const he_plan* plan, uint32_t limbs, uint32_t outputs, int 
     return HE_OK;
 }
 
+int he_test_i8_form(const he_i8_layer* layer, uint32_t limbs, uint32_t outputs, int packed, uint32_t* groups, uint32_t* run, uint32_t* form) {
+    if (!layer || !groups || !run || !form || outputs < 1 || outputs > 64) return HE_ERR_ARG;
+    if (int rc = check_level(layer->ctx, limbs, 1)) return rc;
+    const I8Form f = i8_form(layer, limbs, outputs > 32 ? 2 : outputs > 16 ? 1 : 0, packed != 0);
+    *groups = f.groups;
+    *run = f.run;
+    *form = f.past_caches ? (u32)HE_FORM_PAST_CACHES : 0u;
+    return HE_OK;
+}
+
 // Which arithmetic the transforms of limbs below 2^50 use from now on: integer butterflies only (1), or the
 // double-precision ones (0, the state a context is created in).
 int he_test_integer_transforms(he_ctx* ctx, int integer_only) {

@@ -596,6 +596,13 @@ int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed) {
     return HE_OK;
 }
 
+I8Form i8_form(const he_i8_layer* l, u32 limbs, u32 cls, bool packed) {
+    const he_ctx* ctx = l->ctx;
+    const Launch k = packed ? class_launch<u32>(ctx, l, limbs, cls) : class_launch<u64>(ctx, l, limbs, cls);
+    return I8Form{l->class_begin[cls + 1] - l->class_begin[cls], k.run,
+                  stores_stream(l->n_read, l->n_out, limbs, ctx->N, packed ? sizeof(u32) : sizeof(u64))};
+}
+
 void fill_i8_limb(I8Limb& c, u64 q) {
     u32 bits = 0;
     while (q >> bits) bits++;

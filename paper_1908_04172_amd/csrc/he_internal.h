@@ -290,6 +290,11 @@ int launch_i8(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const u64* ct_in, co
               hipStream_t s);
 int launch_i8_32(he_ctx* ctx, const he_i8_layer* l, u32 limbs, const u32* ct_in, const u32* token, const u64* bias, u32* out, u32 accumulate,
                  hipStream_t s);
+struct I8Form {
+    u32 groups, run;  // of a class; of them those that a workgroup runs through
+    bool past_caches;
+};
+I8Form i8_form(const he_i8_layer* l, u32 limbs, u32 cls, bool packed);
 // sampling from decoded slots (he_sample.hip)
 constexpr u32 SAMPLE_MAX_TOKENS = 32768;
 int launch_sample(he_ctx* ctx, const double* slots, u32 n, u32 n_slots, u32 parts, const double* temperature, const u32* top_k, const double* top_p,

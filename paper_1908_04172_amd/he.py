@@ -37,7 +37,7 @@ EXPORTS = [
     "he_host_mac_accumulate", "he_host_mac_accumulate_add", "he_host_mac_accumulate_lazy", "he_test_mac_for_rescale", "he_measure_rate",
     "he_host_barrett64", "he_host_shoup32", "he_host_mac_digits", "he_host_digit_reduce", "he_test_mac_groups_per_workgroup", "he_test_mac_form", "he_host_ntt_forward_fp64", "he_host_ntt_expand_fp64", "he_host_ntt_inverse_fp64", "he_test_integer_transforms", "he_square_relin_workspace_bytes", "he_ct_square_relin", "he_pack32", "he_unpack32", "he_ct_pt_mac32", "he_ct_pt_add32", "he_rescale32", "he_ntt_fwd32", "he_ntt_inv32",
     "he_i8_layer_create", "he_i8_layer_destroy", "he_i8_workspace_bytes", "he_ct_i8_mac", "he_ct_i8_mac32",
-    "he_sample_slots", "he_host_i8_mac",
+    "he_sample_slots", "he_host_i8_mac", "he_test_i8_form",
 ]
 
 _lib = None
@@ -110,6 +110,7 @@ def lib():
         "he_i8_layer_destroy": (i32, [vp]),
         "he_i8_workspace_bytes": (i32, [vp, u32, u32, ctypes.POINTER(sz)]),
         "he_ct_i8_mac": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
+        "he_test_i8_form": (i32, [vp, u32, u32, i32, ctypes.POINTER(u32), ctypes.POINTER(u32), ctypes.POINTER(u32)]),
         "he_host_i8_mac": (u64, [vp, vp, sz, u64, u64, u64, u64, i32]),
         "he_sample_slots": (i32, [vp, vp, u32, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp]),
         "he_ct_i8_mac32": (i32, [vp, vp, u32, vp, vp, vp, vp, u32, vp, sz, vp]),
@@ -586,6 +587,12 @@ class I8Layer:
         b = ctypes.c_size_t()
         _check(lib().he_i8_workspace_bytes(self._h, limbs, flags, ctypes.byref(b)), "he_i8_workspace_bytes")
         return int(b.value)
+
+    def form(self, limbs: int, outputs: int, packed: bool = False):
+        """he_test_i8_form: (groups, groups of a workgroup, FORM_* bits)."""
+        v = [ctypes.c_uint32() for _ in range(3)]
+        _check(lib().he_test_i8_form(self._h, limbs, outputs, int(packed), *(ctypes.byref(x) for x in v)), "he_test_i8_form")
+        return tuple(int(x.value) for x in v)
 
     def close(self):
         if getattr(self, "_h", None):
