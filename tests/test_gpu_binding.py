@@ -37,3 +37,19 @@ def test_conjugated_and_negated_tensors(he):
     want = ctx.sample_slots(flipped, u, parts=he.SLOTS_COMPLEX)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.equal(ctx.encode_vector(lazy.resolve_conj(), 2.0**20), ctx.encode_vector(flipped, 2.0**20))
+
+
+def test_top_k_is_unsigned(he):
+    """Numbers of 2^31 and more, which an int32 tensor holds as negative ones, are more than any row has: off, as 0 is."""
+    ctx = he.Context(10, wl.modulus_chain([40], 1 << 10))
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    for n in (50, 1000):                                            # (rows that are ranked at once, and rows with histograms)
+        slots = torch.view_as_complex(torch.randn((n, 512, 2), dtype=torch.float64, device="cuda", generator=gen))
+        u = torch.rand(512, dtype=torch.float64, device="cuda", generator=gen)
+        p = torch.full((512,), 0.9, dtype=torch.float64, device="cuda")
+        want, filtered = ctx.sample_slots(slots, u), ctx.sample_slots(slots, u, top_p=p)
+        for k in (-1, -2**31, 2**31 - 1, n, 0):
+            top_k = torch.full((512,), k, dtype=torch.int32, device="cuda")
+            for got, expect in ((ctx.sample_slots(slots, u, top_k=top_k), want), (ctx.sample_slots(slots, u, top_k=top_k, top_p=p), filtered)):
+                assert all(torch.equal(a, b) for a, b in zip(got, expect)), (n, k)
