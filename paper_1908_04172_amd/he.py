@@ -278,7 +278,9 @@ class Context:
         import torch
         n, half = slots.shape
         rows = uniform.numel()
-        assert slots.dtype == torch.complex128 and half == self.N // 2 and rows % parts == 0
+        assert slots.dtype == torch.complex128 and half == self.N // 2
+        n_slots, rest = divmod(rows, parts) if parts > 0 else (0, 0)  # (other numbers of parts are the library's to refuse)
+        assert rest == 0
         for t in (uniform, temperature, top_p, min_p, log_prob):
             assert t is None or (t.dtype == torch.float64 and t.shape == (rows,))
         assert top_k is None or (top_k.dtype == torch.int32 and top_k.shape == (rows,))
@@ -287,7 +289,7 @@ class Context:
         if log_prob is None:
             log_prob = torch.empty(rows, dtype=torch.float64, device=slots.device)
         assert out.dtype == torch.int32 and out.shape == (rows,)
-        _check(lib().he_sample_slots(self._h, _dev_ptr(slots, "slots"), n, rows // parts, parts, _dev_ptr(temperature, "temperature"),
+        _check(lib().he_sample_slots(self._h, _dev_ptr(slots, "slots"), n, n_slots, parts, _dev_ptr(temperature, "temperature"),
                                      _dev_ptr(top_k, "top_k"), _dev_ptr(top_p, "top_p"), _dev_ptr(min_p, "min_p"),
                                      _dev_ptr(uniform, "uniform"), _dev_ptr(out, "tokens"), _dev_ptr(log_prob, "log_prob"), _stream()),
                "he_sample_slots")

@@ -53,3 +53,12 @@ def test_top_k_is_unsigned(he):
             top_k = torch.full((512,), k, dtype=torch.int32, device="cuda")
             for got, expect in ((ctx.sample_slots(slots, u, top_k=top_k), want), (ctx.sample_slots(slots, u, top_k=top_k, top_p=p), filtered)):
                 assert all(torch.equal(a, b) for a, b in zip(got, expect)), (n, k)
+
+
+def test_rows_per_slot_are_one_or_two(he):
+    ctx = he.Context(10, wl.modulus_chain([40], 1 << 10))
+    slots = torch.zeros((4, 512), dtype=torch.complex128, device="cuda")
+    for parts in (0, 3, -1):
+        with pytest.raises(he.HeError) as e:
+            ctx.sample_slots(slots, torch.zeros(6, dtype=torch.float64, device="cuda"), parts=parts)
+        assert e.value.status == -1, parts
