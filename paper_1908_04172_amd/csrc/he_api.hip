@@ -1344,8 +1344,6 @@ uint64_t he_host_mac_digits(const uint64_t* x, const uint64_t* w, size_t n, uint
     return he_host_digit_reduce(sums, q, addend, form);
 }
 
-// What a fused layer's MAC hands to its rescale kernel on a kept limb: unreduced where the limb takes that and the sum is taken
-// in one part, else canonical (longer sums are added up part by part).
 // An output of an int8 layer as the device forms it (he_test.h): digits, their sums, and the end; packed: the 32-bit form.
 uint64_t he_host_i8_mac(const uint64_t* x, const int8_t* w, size_t n, uint64_t q, uint64_t scale, uint64_t token, uint64_t bias, int packed) {
     I8Limb c;
@@ -1366,6 +1364,8 @@ uint64_t he_host_i8_mac(const uint64_t* x, const int8_t* w, size_t n, uint64_t q
     return i8_token(r, token, h_shoup(token, q), bias, c);
 }
 
+// What a fused layer's MAC hands to its rescale kernel on a kept limb: unreduced where the limb takes that and the sum is taken
+// in one part, else canonical (longer sums are added up part by part).
 uint64_t he_host_mac_accumulate_lazy(const uint64_t* x, const uint64_t* w, size_t n, uint64_t q, uint64_t addend) {
     const LimbConst c = host_const(q);
     const u32 lazy = c.fp_ok ? 2 : mac_lazy(c, HE_MAX_LOG2N - 1);

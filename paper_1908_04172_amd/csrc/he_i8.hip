@@ -66,11 +66,7 @@ struct I8Args {
     u32 accumulate;
 };
 
-template <typename T>
-__device__ __forceinline__ T uniform_load(const T* p) {  // read-only, workgroup-uniform data: a scalar load
-    return *(const __attribute__((address_space(4))) T*)(p);
-}
-__device__ __forceinline__ I8Group load_group(const I8Group* p) {
+__device__ __forceinline__ I8Group load_group(const I8Group* p) {  // (read-only, the same for the whole workgroup: a scalar load)
     typedef u32 u32x8 __attribute__((ext_vector_type(8)));
     const u32x8 v = *(const __attribute__((address_space(4))) u32x8*)(p);
     return I8Group{v[0], v[1], v[2], v[3], v[4], {0, 0, 0}};
@@ -314,7 +310,7 @@ __device__ __forceinline__ void whole_body(const I8Args<V>& a, const LimbConst& 
             fin.template with_kind<ND>([&](auto exact, auto token) {
 #pragma unroll
                 for (int i = 0; i < 4 * RT; i++) {
-                        if (4 * (u32)i >= g.count) break;
+                    if (4 * (u32)i >= g.count) break;
                     const u32 mine = 4 * i + quarter;
                     if (mine < g.count) {
                         u64 y[2][2];
@@ -529,7 +525,6 @@ __global__ void __launch_bounds__(THREADS, 2) i8_split_kernel(LimbTable lt, I8Li
     else split_body<V, STREAM, 2>(a, c, l, g, at.part, at.row, ends, lds, ct_list);
 }
 
-template <typename V>
 u32 class_count(const he_i8_layer* l, u32 cls) { return l->class_begin[cls + 1] - l->class_begin[cls]; }
 
 // How a class is launched: the groups that a workgroup takes, and the workgroups.
@@ -539,7 +534,7 @@ struct Launch {
 };
 template <typename V>
 Launch class_launch(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls) {
-    const u64 rows = 2 * limbs, count = class_count<V>(l, cls);
+    const u64 rows = 2 * limbs, count = class_count(l, cls);
     if (cls >= 2) return Launch{1, count * (ctx->N / split_slots<V>()) * rows};
     Launch k{WHOLE_RUN, 0};
     auto blocks = [&] { return (count + k.run - 1) / k.run * (ctx->N / whole_slots<V>()) * rows; };
@@ -551,7 +546,7 @@ Launch class_launch(const he_ctx* ctx, const he_i8_layer* l, u32 limbs, u32 cls)
 template <typename V, bool STREAM, int CLS>
 int launch_class(he_ctx* ctx, I8Args<V> a, const he_i8_layer* l, hipStream_t s) {
     a.first = l->class_begin[CLS];
-    a.n_groups = class_count<V>(l, CLS);
+    a.n_groups = class_count(l, CLS);
     if (a.n_groups == 0) return HE_OK;
     const Launch k = class_launch<V>(ctx, l, a.limbs, CLS);
     const dim3 grid((u32)k.blocks), block(THREADS);
@@ -599,7 +594,7 @@ int check_i8_launch(he_ctx* ctx, const he_i8_layer* l, u32 limbs, bool packed) {
 I8Form i8_form(const he_i8_layer* l, u32 limbs, u32 cls, bool packed) {
     const he_ctx* ctx = l->ctx;
     const Launch k = packed ? class_launch<u32>(ctx, l, limbs, cls) : class_launch<u64>(ctx, l, limbs, cls);
-    return I8Form{l->class_begin[cls + 1] - l->class_begin[cls], k.run,
+    return I8Form{class_count(l, cls), k.run,
                   stores_stream(l->n_read, l->n_out, limbs, ctx->N, packed ? sizeof(u32) : sizeof(u64))};
 }
 

@@ -153,11 +153,12 @@ struct he_plan {
 // ---- int8 layers (he_i8.hip)
 constexpr u32 I8_CLASSES = 3;          // groups of up to 16, 32 and 64 outputs
 constexpr u32 I8_MAX_TERMS = 131071;   // of an output: sums of so many products of at most 2^14 stay below 2^31
-// Outputs that read the same ciphertexts in the same order.
+// Outputs that follow one another, summed over one list of ciphertexts: what all of them read in the same order, or the union of what
+// neighbouring windows read, with weights of zero where an output lacks one.
 struct I8Group {
     u32 out0, count;
-    u32 n_terms;   // of each output
-    u32 list;      // where the ciphertexts of the terms start in he_i8_layer::lists_dev, in blocks of 32 terms
+    u32 n_terms;   // of the list
+    u32 list;      // where it starts in he_i8_layer::lists_dev, in blocks of 32 terms
     u32 table;     // where the weights start in he_i8_layer::table_dev, in units of 512 bytes
     u32 pad[3];
 };
@@ -169,7 +170,7 @@ struct he_i8_layer {
     int device;
     u32 n_in, n_out, n_terms;
     u32 n_read;                       // inputs that some term names
-    u32 class_begin[I8_CLASSES + 1];  // groups sorted by the tiles of 32 outputs that they take
+    u32 class_begin[I8_CLASSES + 1];  // the groups by class; groups without terms are in the last one
     I8Limbs limbs;
     I8Group* groups_dev;
     u32* lists_dev;    // the groups' ciphertexts, padded to blocks of 32 with the last one
