@@ -386,10 +386,13 @@ int launch_sample(he_ctx* ctx, const double* slots, u32 n, u32 n_slots, u32 part
                   const double* min_p, const double* uniform, int32_t* tokens, double* log_prob, hipStream_t s) {
     SampleArgs a{slots, temperature, top_p, min_p, uniform, top_k, tokens, log_prob, (size_t)ctx->N, n, n_slots * parts, parts, 3, 0};
     // Eight rows, which are a cache line (real parts) or half of one, as far as the registers hold them and there are rows enough for every compute
-    // unit.  A workgroup is no larger than it must be, so that one loads while another searches: rows of 1025 tokens and more take 32 per
-    // thread of 512 (n = 8192, 4096 rows, top-k and top-p: 200 us, with 16 per thread of 1024 295), shorter ones 16 (n = 1000: 50 us, 65 with 32).
+    // unit.  A workgroup is no larger than it must be, so that one loads while another searches.  Its threads take 16 tokens each up to n = 2048 and 32
+    // beyond, where fewer rows would leave too little of a line (4096 rows, top-k and top-p: n = 2048 70 us, 92 with 32; n = 2049 93, 103 with 16; n = 8192
+    // 238, 287 with 16; from 1025 to 2048 tokens 16 were as fast or faster at every number of rows from 256 to 4096, by up to 43 %; between 2049 and 4096
+    // anything from 24 % faster to 11 % slower).  Rows beyond 16384 tokens need 1024 threads, whose registers leave one workgroup to a compute unit and three of a
+    // thread's weights in scratch memory (512 rows, top-k and top-p: n = 16384 87 us, n = 16385 157, n = 32768 206).
     // Where few rows leave compute units idle, a thread takes eight.
-    const u32 most = n > 1024 ? 32 : 16, widest = n > 512 * 32 ? 1024 : 512;
+    const u32 most = n > 2048 ? 32 : 16, widest = n > 512 * 32 ? 1024 : 512;
     while (a.rows_log > 0 && ((widest >> a.rows_log) * most < n || (a.rows >> a.rows_log) < 256)) a.rows_log--;
     const bool few = (a.rows >> a.rows_log) < 256;
     u32 T = 256;

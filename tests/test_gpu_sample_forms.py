@@ -9,7 +9,7 @@ from test_gpu_sample import check, contexts, he, random_params  # noqa: E402,F40
 pytestmark = pytest.mark.gpu
 
 
-# (a workgroup of 512 threads holds 16 tokens each up to n = 1024 and 32 beyond, so eight rows up to 2048, four up to 4096, two up to 8192 and
+# (a workgroup of 512 threads holds 16 tokens each up to n = 2048 and 32 beyond, so eight rows up to 1024, four up to 4096, two up to 8192 and
 # one up to 16384; then 1024 threads; and fewer rows while there are not 256 workgroups)
 @pytest.mark.parametrize("n,log2N,n_slots,parts", [(1024, 12, 2048, 1), (1025, 12, 2047, 1), (2048, 12, 2048, 1), (2049, 11, 1024, 1), (4096, 10, 511, 2),
                                                    (4097, 10, 512, 1), (8192, 10, 257, 2), (8193, 10, 256, 1), (16384, 10, 256, 1),
