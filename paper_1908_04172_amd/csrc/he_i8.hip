@@ -20,11 +20,11 @@
 // The end of an output, two products by constants of the output and one reduction: I8Channel in he_arith.h.
 //
 // What bounds it: the first form the vector ALU, whose instructions are 30 % transposition and 70 % ends (a 16x16x8 map, 3x3x16, N = 2^13, L = 3,
-// with tokens: 833 us for 2.4 GB; a 28x28 image, 5x5x5, L = 4: 205 us for 0.79 GB, 3.8 TB/s); long sums over few groups the inputs' way from memory (845 -> 100 at
-// 2^13, L = 4: 122 us for 0.50 GB, 4.1 TB/s; he_ct_pt_mac's products alone 345 us); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2: 101 us),
-// of long ones the products, transposition and LDS in turn (1024 -> 1024 packed: 115 us, 1.2 int8 POP/s).
-// Groups of the second form hold 64 outputs and not 128, whose sums would leave one workgroup per compute unit, with its ends in the open: 256 -> 1000 106 and
-// 150 us, 845 -> 100 142 and 161, 1024 -> 1024 packed 134 and 140.
+// with tokens: 842 us for 2.4 GB; a 28x28 image, 5x5x5, L = 4: 206 us for 0.79 GB, 3.8 TB/s); long sums over few groups the inputs' way from memory (845 -> 100 at
+// 2^13, L = 4: 122 us for 0.50 GB, 4.0 TB/s; with the rescale 175 us, he_ct_pt_mac 409); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2:
+// 102 us), of long ones the products, transposition and LDS in turn (1024 -> 1024 packed: 117 us, 1.2 int8 POP/s).
+// Groups of the second form hold 64 outputs and not 128, whose sums would leave one workgroup per compute unit, with its ends in the open: with 128, the ends as
+// they then were, 256 -> 1000 took 1.41 times as long, 845 -> 100 1.13 times, 1024 -> 1024 packed 1.04 times.
 #include <string.h>
 
 #include <algorithm>
@@ -41,8 +41,10 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 constexpr u32 THREADS = 256;
-constexpr u32 WHOLE_RUN = 16;        // groups that a workgroup of the first form runs through, at most (the 16x16x8 map 968 us, 1016 with two)
-constexpr u64 MIN_WORKGROUPS = 2048; // ... while the launch keeps at least this many workgroups
+// Groups that a workgroup of the first form runs through, at most (the 16x16x8 map 842 us, with runs of 8, 4, 2 and 1 830, 856, 908 and 1033), and
+// the workgroups that a launch keeps (the 28x28 image 208 us; with 1024 of them 243, with 4096 208, with 8192 229).
+constexpr u32 WHOLE_RUN = 16;
+constexpr u64 MIN_WORKGROUPS = 2048;
 
 // slots of a workgroup, in units of eight bytes: 32 per wavefront in the first form, 64 in all in the second
 template <typename V>
@@ -661,12 +663,15 @@ struct Merged {
 };
 
 // The classes of groups: one or two tiles of 16 in the first form, two of 32 in the second.  (One tile is half the products: 845 -> 10 at N = 2^13, L = 4,
-// 78.9 us, 80.4 with two.)
+// 79.9 us, 80.2 with two.)
 u32 class_of(u32 count) { return count > 32 ? 2 : count > 16 ? 1 : 0; }
 u32 blocks_of(u32 count, u32 terms) { return count > 32 ? (terms + 63) / 64 * 2 : (terms + 31) / 32; }
 
-// What a group costs, in cycles of a SIMD per 32 slots, as far as it matters for what to merge: loads, transposition and products of a block
-// of terms, the ends of four outputs, and its start.
+// What a group costs, as far as it matters for what to merge: loads, transposition and products of a block of terms, the ends of four outputs, and its
+// start.  Only the proportions count.  Layers of 256 such groups (N = 2^13, moduli of 60 and 50 bits, inputs from the caches) take 780 (up to 16 outputs) and
+// 1000 cycles of a SIMD per block and 32 slots, 530 per four outputs and 450 to start.  What is decided by it hangs little on them: six
+// convolutions with each constant halved or doubled, or the start four times as dear or free, took from 4 % less time to 4 % more; unmerged 11 to 40 % more, but for
+// one whose windows are too many outputs to merge.
 u32 group_cost(u32 count, u32 terms) { return blocks_of(count, terms) * (count > 16 ? 700 : 600) + (count + 3) / 4 * 400 + 250; }
 
 struct LayerBuilder {

@@ -12,9 +12,10 @@
 // that has more than LIST weights, bins of a 64th of it; what is left is ranked by comparing all with all.  Rows of up to LIST tokens
 // are ranked at once.  The token is found by the running sum in the order of the indices.
 //
-// What bounds it: long rows the loads, of which a workgroup of two rows takes 16 bytes of every line, and the vector ALU in turn (8192 tokens, 4096 rows, top-k and
-// top-p: 200 us for 268 MB, 125 without filters); shorter ones the histogram's atomics and the meetings of the wavefronts (1000 tokens, 4096 rows, all filters: 48 us, 22 without); few rows and
-// short ones latency (5003 tokens, 37 rows: 26 us; ten tokens, 2048 rows: 6 us).
+// What bounds it: long rows the loads, of which a workgroup of two rows takes 16 bytes of every line, and the vector ALU in turn (8192 tokens, 4096 rows as 2048
+// slots, top-k and top-p: 207 us for 268 MB, 144 without filters); shorter ones the histogram's atomics and the meetings of the wavefronts (1000
+// tokens, 4096 rows, all filters: 49 us, 22 without); few rows and short ones latency (5003 tokens, 37 rows, top-p and min-p: 28 us, 19 without; ten tokens, 2048
+// rows: 6.3 us, with the exponentials of eight tokens per thread, which any n takes).
 #include <math.h>
 
 #include <algorithm>
