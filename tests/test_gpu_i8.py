@@ -1,5 +1,5 @@
 """Layers of 8-bit integer weights (he_ct_i8_mac, he_ct_i8_mac32) at the sizes where they can go wrong: output counts around the
-tiles of 32 and the groups of 128, term counts around the blocks of 32 and up to the longest sum, moduli of every width, extreme
+tiles of 32 and the groups of 64, term counts around the blocks of 32 and up to the longest sum, moduli of every width, extreme
 residues and weights, and every combination of scales and bias.  Exact residues, against the oracle and Python integers."""
 import numpy as np
 import pytest
