@@ -150,8 +150,8 @@ def _dev_ptr(t, name: str) -> Optional[int]:
     global _Tensor, _DTYPES
     if _Tensor is None:
         import torch
-        _Tensor = torch.Tensor
         _DTYPES = {torch.int64: False, torch.int32: False, torch.uint8: False, torch.float64: True, torch.complex128: True}
+        _Tensor = torch.Tensor  # (last: another thread that finds it finds the dtypes too)
     if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a contiguous CUDA tensor")
     lazy = _DTYPES.get(t.dtype)
