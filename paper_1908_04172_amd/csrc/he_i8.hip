@@ -21,7 +21,7 @@
 //
 // What bounds it: the first form the vector ALU, whose instructions are 30 % transposition and 70 % ends (a 16x16x8 map, 3x3x16, N = 2^13, L = 3,
 // with tokens: 842 us for 2.4 GB; a 28x28 image, 5x5x5, L = 4: 206 us for 0.79 GB, 3.8 TB/s); long sums over few groups the inputs' way from memory (845 -> 100 at
-// 2^13, L = 4: 122 us for 0.50 GB, 4.0 TB/s; with the rescale 175 us, he_ct_pt_mac 409); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2:
+// 2^13, L = 4: 122 us for 0.50 GB, 4.0 TB/s; with the rescale 173 us, he_ct_pt_mac 411); many outputs of short sums the ends (256 -> 1000 at 2^12, L = 2:
 // 102 us), of long ones the products, transposition and LDS in turn (1024 -> 1024 packed: 117 us, 1.2 int8 POP/s).
 // Groups of the second form hold 64 outputs and not 128, whose sums would leave one workgroup per compute unit, with its ends in the open: with 128, the ends as
 // they then were, 256 -> 1000 took 1.41 times as long, 845 -> 100 1.13 times, 1024 -> 1024 packed 1.04 times.
@@ -41,8 +41,8 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 constexpr u32 THREADS = 256;
-// Groups that a workgroup of the first form runs through, at most (the 16x16x8 map 842 us, with runs of 8, 4, 2 and 1 830, 856, 908 and 1033), and
-// the workgroups that a launch keeps (the 28x28 image 208 us; with 1024 of them 243, with 4096 208, with 8192 229).
+// Groups that a workgroup of the first form runs through, at most (the 16x16x8 map 845 us, with runs of 8, 4, 2 and 1 829, 858, 908 and 1035), and
+// the workgroups that a launch keeps (the 28x28 image 209 us; with 1024 of them 242, with 4096 208, with 8192 229).
 constexpr u32 WHOLE_RUN = 16;
 constexpr u64 MIN_WORKGROUPS = 2048;
 
@@ -663,7 +663,7 @@ struct Merged {
 };
 
 // The classes of groups: one or two tiles of 16 in the first form, two of 32 in the second.  (One tile is half the products: 845 -> 10 at N = 2^13, L = 4,
-// 79.9 us, 80.2 with two.)
+// 79.4 us, 80.4 with two.)
 u32 class_of(u32 count) { return count > 32 ? 2 : count > 16 ? 1 : 0; }
 u32 blocks_of(u32 count, u32 terms) { return count > 32 ? (terms + 63) / 64 * 2 : (terms + 31) / 32; }
 

@@ -221,9 +221,9 @@ int check_mac_launch(he_ctx* ctx, const he_plan* plan, u32 limbs, int pt_kind);
 // lines costs 256 groups of 16 outputs of one term, N = 2^13, L = 4, 800 us against 540, the layer 30 -> 120 at 2^14, L = 8 (60 + 240 MiB) 322
 // against 301.  What does fit is read from the cache by the call that adds to it or rescales it: the layer 100 -> 200 at 2^13,
 // L = 4 (50 + 100 MiB) 174 us, 181 past the caches; 20 -> 300 with a second call that adds, then the rescale, 296 and 326.
-// Int8 layers go by the same line: 113 -> 37 at 2^14, L = 8 (226 + 74 MiB) 93 us through the caches and 90 past them, 845 -> 100 at 2^13, L = 4
-// (422 + 50 MiB) 128 and 125.  What fits stays for the call that reads it: 256 -> 1000 at 2^12, L = 2 (32 + 125 MiB) with its rescale 174 and 177, with
-// HE_ACCUMULATE 141 both; the product alone would be faster past them, 108 and 91.
+// Int8 layers go by the same line: 113 -> 37 at 2^14, L = 8 (226 + 74 MiB) 91 us through the caches and 89 past them, 845 -> 100 at 2^13, L = 4
+// (422 + 50 MiB) 127 and 123.  What fits stays for the call that reads it: 256 -> 1000 at 2^12, L = 2 (32 + 125 MiB) with its rescale 167 and 171, with
+// HE_ACCUMULATE 141 both; the product alone would be faster past them, 103 and 85.
 inline bool stores_stream(u32 n_read, u32 n_out, u32 limbs, u32 N, size_t residue_bytes) {
     const u64 per_ct = (u64)2 * limbs * N * residue_bytes, out = n_out * per_ct;
     return out > L2_BYTES && n_read * per_ct + out > MEMORY_CACHE_BYTES;

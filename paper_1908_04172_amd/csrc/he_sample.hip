@@ -388,10 +388,10 @@ int launch_sample(he_ctx* ctx, const double* slots, u32 n, u32 n_slots, u32 part
     SampleArgs a{slots, temperature, top_p, min_p, uniform, top_k, tokens, log_prob, (size_t)ctx->N, n, n_slots * parts, parts, 3, 0};
     // Eight rows, which are a cache line (real parts) or half of one, as far as the registers hold them and there are rows enough for every compute
     // unit.  A workgroup is no larger than it must be, so that one loads while another searches.  Its threads take 16 tokens each up to n = 2048 and 32
-    // beyond, where fewer rows would leave too little of a line (4096 rows, top-k and top-p: n = 2048 70 us, 92 with 32; n = 2049 93, 103 with 16; n = 8192
-    // 238, 287 with 16; from 1025 to 2048 tokens 16 were as fast or faster at every number of rows from 256 to 4096, by up to 43 %; between 2049 and 4096
+    // beyond, where fewer rows would leave too little of a line (4096 rows, top-k and top-p: n = 2048 74 us, 97 with 32; n = 2049 98, 109 with 16; n = 8192
+    // 238, 286 with 16; from 1025 to 2048 tokens 16 were as fast or faster at every number of rows from 256 to 4096, by up to 43 %; between 2049 and 4096
     // anything from 24 % faster to 11 % slower).  Rows beyond 16384 tokens need 1024 threads, whose registers leave one workgroup to a compute unit and three of a
-    // thread's weights in scratch memory (512 rows, top-k and top-p: n = 16384 87 us, n = 16385 157, n = 32768 206).
+    // thread's weights in scratch memory (512 rows, top-k and top-p: n = 16384 87 us, n = 16385 160, n = 32768 205).
     // Where few rows leave compute units idle, a thread takes eight.
     const u32 most = n > 2048 ? 32 : 16, widest = n > 512 * 32 ? 1024 : 512;
     while (a.rows_log > 0 && ((widest >> a.rows_log) * most < n || (a.rows >> a.rows_log) < 256)) a.rows_log--;
